@@ -185,7 +185,7 @@ def prepare(case, seed):
     # a few keys get most of the attention
     weight = torch.rand((B, Hkv, T), generator=g, device="cuda").pow_(8).mul_(50.0)
     s.update(k_cache=bf(pages, P, Hkv, D), page_table=_dev(table), kv_len=_dev(lens), seen=_dev(seen),
-             fixed_len=_dev(fixed), weight=weight, position=position, weight_out=torch.zeros_like(weight))
+             max_kv_len=int(lens.max()), fixed_len=_dev(fixed), weight=weight, position=position, weight_out=torch.zeros_like(weight))
     if case["kind"] == "weights":
         N, Hq = case["N"], case["Hq"]
         alen = rng.integers(1, case["amax"] + 1, size=B).astype(np.int32)
@@ -307,7 +307,8 @@ def run(state):
             import paper_2602_21224_amd as T
             return T.kv_accumulate_weights(
                 s["q"], s["lse"], s["k_cache"], s["page_table"], s["kv_len"], s["accept_idx"], s["accept_len"],
-                s["weight"], s["position"], s["seen"], fixed_len=s["fixed_len"], weight_out=s["weight_out"])
+                s["weight"], s["position"], s["seen"], max_kv_len=s["max_kv_len"], fixed_len=s["fixed_len"],
+                weight_out=s["weight_out"])
         return _plain_weights(s)
     if own:
         import paper_2602_21224_amd as T
@@ -316,8 +317,9 @@ def run(state):
                                          dtype=torch.uint8, device="cuda")
         weight, position, kept = T.kv_evict(
             s["weight"], s["position"], s["k_cache"], s["v_cache"], s["page_table"], s["kv_len"], s["seen"],
-            budget=c["budget"], recent=c["recent"], fixed_len=s["fixed_len"], weight_out=s["weight_out"],
-            position_out=s["position_out"], kept_len=s["kept_len"], workspace=s["workspace"])
+            max_kv_len=s["max_kv_len"], budget=c["budget"], recent=c["recent"], fixed_len=s["fixed_len"],
+            weight_out=s["weight_out"], position_out=s["position_out"], kept_len=s["kept_len"],
+            workspace=s["workspace"])
         return s["k_cache"], s["v_cache"], weight, position, kept
     return _plain_evict(s)
 
