@@ -7,7 +7,7 @@
  * under a tree-shaped attention mask (§2.1; §8 cites SpecInfer's tree
  * masking), accepts one path of the tree and produces a bonus token (§5.3),
  * decoding greedily (§7.1: temperature 0), over a paged KV cache (§7.1).
- * The three calls below are that step's data-parallel part:
+ * Three calls are that step's data-parallel part:
  *
  *   tree_verify_attention  every node's query heads attend to the sequence's
  *                          committed prefix and to the node's own root path;
@@ -234,6 +234,135 @@ TV_API int kv_compact_accepted(const uint16_t *k_tree, const uint16_t *v_tree, u
                                const int32_t *kv_len, const int32_t *accept_idx,
                                const int32_t *accept_len, int B, int N, int Hkv, int D, int P,
                                int max_pages, int num_pages, hipStream_t stream);
+
+/* ------------------------------------------------------------------------
+ * tree_verify_attention_shared
+ *
+ * tree_verify_attention for batches whose sequences begin with the same
+ * tokens (a system prompt, a document): the sequences of a group share the
+ * cache rows of their first tokens, and each shared K/V row is read once for
+ * all query rows of the group instead of once per sequence. What is computed
+ * is tree_verify_attention's function of the same arguments (§2.1, §7.1: its
+ * declaration above gives formulas, layouts and limits); which keys are taken
+ * together changes roundings only.
+ *
+ *   groups       number of groups, 0 <= groups <= 256; with 0 the two arrays
+ *                may be NULL and every sequence is attended by itself
+ *   group_start  [groups + 1] int32, ascending: group s is the sequences
+ *                group_start[s] .. group_start[s + 1] - 1. Sequences before the
+ *                first group or behind the last one are attended by themselves.
+ *   shared_len   [groups] int32: for every t < shared_len[s] all sequences of
+ *                group s that have nodes hold position t in the same page,
+ *                page_table[b][t / P]. Any value >= 0; what exceeds a
+ *                sequence's kv_len is not used.
+ *   workspace    >= tv_shared_attention_workspace_size(...) bytes, 16-byte
+ *                aligned; contents on entry do not matter; clobbered.
+ * A start that is not ascending counts as the largest before it, one outside
+ * [0, B] is clamped. Where the pages of a group's sequences differ below
+ * shared_len, results are unspecified. Calls captured into graphs that may
+ * run at the same time need workspaces of their own.
+ * Supported: as tree_verify_attention, with 0 <= B <= 512.
+ * ------------------------------------------------------------------------ */
+TV_API size_t tv_shared_attention_workspace_size(int B, int N, int Hq, int Hkv, int D, int groups);
+
+TV_API int tree_verify_attention_shared(
+    const uint16_t *q, const uint16_t *k_tree, const uint16_t *v_tree, const uint16_t *k_cache,
+    const uint16_t *v_cache, const int32_t *page_table, const int32_t *kv_len,
+    const int32_t *parent, const int32_t *num_nodes, const int32_t *group_start,
+    const int32_t *shared_len, int groups, int B, int N, int Hq, int Hkv, int D, int P,
+    int max_pages, int num_pages, int max_kv_len, float scale, uint16_t *out, float *lse,
+    void *workspace, size_t workspace_bytes, hipStream_t stream);
+
+/* ------------------------------------------------------------------------
+ * kv_accumulate_weights
+ *
+ * Adds to every cached key the softmax weight that the accepted path's query
+ * heads gave it, per sequence b and KV head g (G = Hq / Hkv), so that
+ * kv_evict can tell which keys matter. Call it after kv_compact_accepted has
+ * put the path's rows into the cache and before kv_len is advanced. With
+ * L = kv_len[b], n = accept_len[b], f = min(fixed_len[b], L):
+ *   p(j, h, t)  = exp(scale * <q[b, accept_idx[b,j], h, :], k_t[g, :]> - lse[b, accept_idx[b,j], h])
+ *   mass(t)     = sum over path rows j < n that see position t (t <= L + j)
+ *                 and heads h of g of p(j, h, t)
+ *   f <= t < L:      weight_out[b,g,t] = weight[b,g,t] + mass(t)
+ *   t < f:           weight_out[b,g,t] = weight[b,g,t]
+ *   L <= t < L + n:  weight_out[b,g,t] = mass(t), position[b,g,t] = seen[b] + (t - L)
+ * Nothing else of weight_out and position is written. Sums are fp32, in a
+ * fixed order. A row whose lse is -inf saw nothing and adds nothing.
+ *
+ *   q            [B, N, Hq, D]            bf16, as given to the attention
+ *   lse          [B, N, Hq]               fp32, as the attention wrote it
+ *   k_cache      [num_pages, P, Hkv, D]   bf16
+ *   page_table [B, max_pages], kv_len [B], accept_idx [B, N], accept_len [B] int32
+ *   seen         [B] int32                tokens that sequence b has committed so
+ *                                         far (kv_len plus what was evicted); the
+ *                                         caller advances it with kv_len
+ *   fixed_len    [B] int32, or NULL (0)   positions below it are never evicted and
+ *                                         their keys are not read
+ *   weight, weight_out  [B, Hkv, T] fp32, T = max_pages * P: may be the same array
+ *   position     [B, Hkv, T] int32        the sequence position of each cached key
+ * A path row whose node id is outside [0, N) is skipped; a position whose page
+ * id is out of range, or at or past T, is left as it is (contract violations).
+ * max_kv_len is a host-side upper bound of kv_len[] that sizes the launch only.
+ * scale <= 0 selects 1/sqrt(D).
+ * Supported: D in {64, 128}; 1 <= N <= 256; Hq % Hkv == 0 and
+ * (Hq / Hkv) * N <= 2048; 0 <= B <= 65535; Hkv <= 65535; P a power of two in
+ * [1, 256]; T <= 2^24. q and k_cache 16-byte aligned.
+ * ------------------------------------------------------------------------ */
+TV_API int kv_accumulate_weights(const uint16_t *q, const float *lse, const uint16_t *k_cache,
+                                 const int32_t *page_table, const int32_t *kv_len,
+                                 const int32_t *accept_idx, const int32_t *accept_len,
+                                 const int32_t *seen, const int32_t *fixed_len,
+                                 const float *weight, int B, int N, int Hq, int Hkv, int D, int P,
+                                 int max_pages, int num_pages, int max_kv_len, float scale,
+                                 float *weight_out, int32_t *position, hipStream_t stream);
+
+/* ------------------------------------------------------------------------
+ * kv_evict
+ *
+ * Shortens every sequence's cache to its budget, per KV head: keeps the keys
+ * that got most attention and moves them together. With L = kv_len[b],
+ * f = min(fixed_len[b], L):
+ *   kept_len[b] = min(L, max(budget, f))
+ * and for each KV head g the kept slots are the first kept_len[b] of slots
+ * 0 .. L-1 in this order:
+ *   slots t < f; then slots with position[b,g,t] >= seen[b] - recent; then the
+ *   others; within each of the three the larger weight[b,g,t] first (ordered as
+ *   tree_argmax_accept orders logits: NaN largest, -0 == +0), lower t on ties.
+ * The evicted slots below kept_len[b], in ascending order, take the K and V
+ * rows, weights and positions of the kept slots at or past kept_len[b], in
+ * ascending order; every other kept slot stays where it is. So slots below
+ * fixed_len are never written (they may be pages that other sequences share),
+ * and only min(evicted, kept past the length) rows move. Keys carry their
+ * positional encoding, so the attention does not depend on slot order;
+ * position tells which token a slot holds.
+ *
+ *   k_cache, v_cache  [num_pages, P, Hkv, D] bf16, rows moved in place; no page
+ *                     id below L of a sequence may occur twice among the slots
+ *                     from fixed_len on, in this or in another sequence
+ *   weight, position  [B, Hkv, T] fp32 / int32, T = max_pages * P
+ *   weight_out, position_out  [B, Hkv, T]: each may be the array it updates;
+ *                     slots below kept_len[b] are written, nothing else
+ *   seen, fixed_len   [B] int32 as for kv_accumulate_weights (fixed_len or NULL)
+ *   kept_len          [B] int32 out: the caller's next kv_len. kv_len and
+ *                     page_table are not modified; pages past kept_len are the
+ *                     caller's again. May not overlap kv_len.
+ *   workspace         >= tv_evict_workspace_size(B, Hkv, max_pages, P) bytes,
+ *                     16-byte aligned; contents on entry do not matter.
+ * A row whose page id is out of range is not moved (contract violation).
+ * max_kv_len is a host-side upper bound of kv_len[] that sizes the launch only.
+ * Supported: 0 <= B <= 65535; Hkv <= 65535; D a multiple of 8, D <= 1024; P a
+ * power of two in [1, 256]; T <= 2^24; budget, recent >= 0. k_cache and
+ * v_cache 16-byte aligned.
+ * ------------------------------------------------------------------------ */
+TV_API size_t tv_evict_workspace_size(int B, int Hkv, int max_pages, int P);
+
+TV_API int kv_evict(const float *weight, const int32_t *position, uint16_t *k_cache,
+                    uint16_t *v_cache, const int32_t *page_table, const int32_t *kv_len,
+                    const int32_t *seen, const int32_t *fixed_len, int B, int Hkv, int D, int P,
+                    int max_pages, int num_pages, int max_kv_len, int budget, int recent,
+                    float *weight_out, int32_t *position_out, int32_t *kept_len, void *workspace,
+                    size_t workspace_bytes, hipStream_t stream);
 
 /* ------------------------------------------------------------------------
  * tv_validate_inputs (debug aid)

@@ -7,6 +7,8 @@ library.
 
 __all__ = ["tree_verify_attention", "tree_argmax_accept", "tree_argmax_accept_noalloc",
            "kv_compact_accepted",
+           "tree_verify_attention_shared", "kv_accumulate_weights", "kv_evict",
+           "shared_attention_workspace_size", "evict_workspace_size",
            "tv_validate_inputs", "tree_build", "tree_resample", "tree_lm_head_argmax_accept",
            "attention_workspace_size", "lm_head_workspace_size",
            "argmax_workspace_size", "tree_build_workspace_size", "abi_version", "load"]

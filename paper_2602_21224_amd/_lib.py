@@ -64,6 +64,17 @@ def load():
     lib.tv_lm_head_workspace_size.restype = sz
     lib.tree_lm_head_argmax_accept.argtypes = [p] * 5 + [i] * 4 + [p] * 5 + [sz, p]
     lib.tree_lm_head_argmax_accept.restype = i
+    lib.tv_shared_attention_workspace_size.argtypes = [i] * 6
+    lib.tv_shared_attention_workspace_size.restype = sz
+    lib.tree_verify_attention_shared.argtypes = ([p] * 11 + [i] * 10 + [ctypes.c_float, p, p, p, sz,
+                                                                        p])
+    lib.tree_verify_attention_shared.restype = i
+    lib.kv_accumulate_weights.argtypes = [p] * 10 + [i] * 9 + [ctypes.c_float, p, p, p]
+    lib.kv_accumulate_weights.restype = i
+    lib.tv_evict_workspace_size.argtypes = [i] * 4
+    lib.tv_evict_workspace_size.restype = sz
+    lib.kv_evict.argtypes = [p] * 8 + [i] * 9 + [p] * 4 + [sz, p]
+    lib.kv_evict.restype = i
     _lib = lib
     return lib
 
@@ -281,6 +292,172 @@ def kv_compact_accepted(k_tree, v_tree, k_cache, v_cache, page_table, kv_len, ac
         _stream(stream))
     _check(st, "kv_compact_accepted")
     return k_cache, v_cache
+
+
+def _want_on(dev, t, name, dtypes, shape=None):
+    """_want, and on the device of the call's first tensor."""
+    _want(t, name, dtypes, shape)
+    if t.device != dev:
+        raise ValueError(f"{name} is on {t.device}, expected {dev}")
+
+
+def _call(what, dev, stream, own, *args):
+    """Call the C entry point on `dev` (made current for the call where it is not) and
+    on `stream`. `own`: tensors that the wrapper allocated, which the caching allocator
+    must not hand out again before another stream than the current one is done with them."""
+    fn = getattr(load(), what)
+    if dev.index != torch.cuda.current_device():
+        with torch.cuda.device(dev):
+            st = fn(*args, _stream(stream))
+    else:
+        st = fn(*args, _stream(stream))
+    if stream is not None:
+        for t in own:
+            t.record_stream(stream)
+    _check(st, what)
+
+
+def shared_attention_workspace_size(B, N, Hq, Hkv, D, groups) -> int:
+    return int(load().tv_shared_attention_workspace_size(B, N, Hq, Hkv, D, groups))
+
+
+def tree_verify_attention_shared(q, k_tree, v_tree, k_cache, v_cache, page_table, kv_len, parent,
+                                 group_start, shared_len, *, max_kv_len: int, num_nodes=None,
+                                 scale: float = 0.0, out=None, lse=None, want_lse: bool = True,
+                                 workspace=None, stream=None):
+    """tree_verify_attention for a batch whose sequences share prefixes: sequences
+    group_start[s] .. group_start[s+1]-1 hold their first shared_len[s] tokens in the
+    same pages, and those rows are read once for the whole group. group_start
+    [groups + 1] and shared_len [groups] are int32 (both None: no groups).
+    Returns (out bf16 [B,N,Hq,D], lse fp32 [B,N,Hq] or None)."""
+    B, N, Hq, D = q.shape
+    Hkv = k_tree.shape[2]
+    num_pages, P = k_cache.shape[0], k_cache.shape[1]
+    max_pages = page_table.shape[1]
+    dev = q.device
+    _want(q, "q", _BF16)
+    _want_on(dev, k_tree, "k_tree", _BF16, (B, N, Hkv, D))
+    _want_on(dev, v_tree, "v_tree", _BF16, (B, N, Hkv, D))
+    _want_on(dev, k_cache, "k_cache", _BF16, (num_pages, P, Hkv, D))
+    _want_on(dev, v_cache, "v_cache", _BF16, (num_pages, P, Hkv, D))
+    _want_on(dev, page_table, "page_table", _I32, (B, max_pages))
+    _want_on(dev, kv_len, "kv_len", _I32, (B,))
+    _want_on(dev, parent, "parent", _I32, (B, N))
+    if num_nodes is not None:
+        _want_on(dev, num_nodes, "num_nodes", _I32, (B,))
+    if (group_start is None) != (shared_len is None):
+        raise ValueError("group_start and shared_len are given together")
+    groups = 0 if shared_len is None else shared_len.shape[0]
+    if groups > 0:
+        _want_on(dev, group_start, "group_start", _I32, (groups + 1,))
+        _want_on(dev, shared_len, "shared_len", _I32, (groups,))
+    own = []
+    if out is None:
+        out = torch.empty((B, N, Hq, D), dtype=torch.bfloat16, device=dev)
+        own.append(out)
+    _want_on(dev, out, "out", _BF16, (B, N, Hq, D))
+    if lse is None and want_lse:
+        lse = torch.empty((B, N, Hq), dtype=torch.float32, device=dev)
+        own.append(lse)
+    if lse is not None:
+        _want_on(dev, lse, "lse", _F32, (B, N, Hq))
+    if workspace is None:
+        need = shared_attention_workspace_size(B, N, Hq, Hkv, D, groups)
+        workspace = torch.empty(max(need, 16), dtype=torch.uint8, device=dev)
+        own.append(workspace)
+    _want_on(dev, workspace, "workspace", _U8)
+    _call("tree_verify_attention_shared", dev, stream, own,
+          _ptr(q), _ptr(k_tree), _ptr(v_tree), _ptr(k_cache), _ptr(v_cache), _ptr(page_table),
+          _ptr(kv_len), _ptr(parent), _ptr(num_nodes), _ptr(group_start if groups else None),
+          _ptr(shared_len if groups else None), groups, B, N, Hq, Hkv, D, P, max_pages, num_pages,
+          int(max_kv_len), float(scale), _ptr(out), _ptr(lse), _ptr(workspace), workspace.numel())
+    return out, lse
+
+
+def kv_accumulate_weights(q, lse, k_cache, page_table, kv_len, accept_idx, accept_len, weight,
+                          position, seen, *, max_kv_len: int, fixed_len=None, weight_out=None,
+                          scale: float = 0.0, stream=None):
+    """Add the attention weight that the accepted path's query rows gave every cached
+    key to `weight` [B, Hkv, max_pages * P] fp32, and enter the path's own keys (weight
+    and `position`, int32 of the same shape). Call it between kv_compact_accepted and
+    advancing kv_len and `seen` [B]. Updates `weight` unless `weight_out` is given, and
+    `position`. Returns (weight_out, position)."""
+    B, N, Hq, D = q.shape
+    num_pages, P, Hkv = k_cache.shape[0], k_cache.shape[1], k_cache.shape[2]
+    max_pages = page_table.shape[1]
+    dev = q.device
+    slots = (B, Hkv, max_pages * P)
+    _want(q, "q", _BF16)
+    _want_on(dev, lse, "lse", _F32, (B, N, Hq))
+    _want_on(dev, k_cache, "k_cache", _BF16, (num_pages, P, Hkv, D))
+    _want_on(dev, page_table, "page_table", _I32, (B, max_pages))
+    _want_on(dev, kv_len, "kv_len", _I32, (B,))
+    _want_on(dev, accept_idx, "accept_idx", _I32, (B, N))
+    _want_on(dev, accept_len, "accept_len", _I32, (B,))
+    _want_on(dev, weight, "weight", _F32, slots)
+    _want_on(dev, position, "position", _I32, slots)
+    _want_on(dev, seen, "seen", _I32, (B,))
+    if fixed_len is not None:
+        _want_on(dev, fixed_len, "fixed_len", _I32, (B,))
+    if weight_out is None:
+        weight_out = weight
+    _want_on(dev, weight_out, "weight_out", _F32, slots)
+    _call("kv_accumulate_weights", dev, stream, (),
+          _ptr(q), _ptr(lse), _ptr(k_cache), _ptr(page_table), _ptr(kv_len), _ptr(accept_idx),
+          _ptr(accept_len), _ptr(seen), _ptr(fixed_len), _ptr(weight), B, N, Hq, Hkv, D, P,
+          max_pages, num_pages, int(max_kv_len), float(scale), _ptr(weight_out), _ptr(position))
+    return weight_out, position
+
+
+def evict_workspace_size(B, Hkv, max_pages, P) -> int:
+    return int(load().tv_evict_workspace_size(B, Hkv, max_pages, P))
+
+
+def kv_evict(weight, position, k_cache, v_cache, page_table, kv_len, seen, *, max_kv_len: int,
+             budget: int, recent: int = 0, fixed_len=None, weight_out=None, position_out=None,
+             kept_len=None, workspace=None, stream=None):
+    """Cut every sequence's cache to max(budget, fixed_len) slots per KV head: the fixed
+    ones, those of the `recent` newest positions, then the heaviest. The kept rows past
+    that length move into the evicted slots below it (K, V, weight, position). Updates
+    the caches, and `weight` and `position` unless other arrays are given for them.
+    Returns (weight_out, position_out, kept_len)."""
+    num_pages, P, Hkv, D = k_cache.shape
+    B, max_pages = page_table.shape
+    dev = k_cache.device
+    slots = (B, Hkv, max_pages * P)
+    _want(k_cache, "k_cache", _BF16)
+    _want_on(dev, v_cache, "v_cache", _BF16, (num_pages, P, Hkv, D))
+    _want_on(dev, page_table, "page_table", _I32, (B, max_pages))
+    _want_on(dev, weight, "weight", _F32, slots)
+    _want_on(dev, position, "position", _I32, slots)
+    _want_on(dev, kv_len, "kv_len", _I32, (B,))
+    _want_on(dev, seen, "seen", _I32, (B,))
+    if fixed_len is not None:
+        _want_on(dev, fixed_len, "fixed_len", _I32, (B,))
+    if weight_out is None:
+        weight_out = weight
+    if position_out is None:
+        position_out = position
+    _want_on(dev, weight_out, "weight_out", _F32, slots)
+    _want_on(dev, position_out, "position_out", _I32, slots)
+    own = []
+    if kept_len is None:
+        kept_len = torch.empty((B,), dtype=torch.int32, device=dev)
+        own.append(kept_len)
+    _want_on(dev, kept_len, "kept_len", _I32, (B,))
+    if kept_len.data_ptr() == kv_len.data_ptr() and B > 0:
+        raise ValueError("kept_len must not be kv_len itself")
+    if workspace is None:
+        need = evict_workspace_size(B, Hkv, max_pages, P)
+        workspace = torch.empty(max(need, 16), dtype=torch.uint8, device=dev)
+        own.append(workspace)
+    _want_on(dev, workspace, "workspace", _U8)
+    _call("kv_evict", dev, stream, own,
+          _ptr(weight), _ptr(position), _ptr(k_cache), _ptr(v_cache), _ptr(page_table),
+          _ptr(kv_len), _ptr(seen), _ptr(fixed_len), B, Hkv, D, P, max_pages, num_pages,
+          int(max_kv_len), int(budget), int(recent), _ptr(weight_out), _ptr(position_out),
+          _ptr(kept_len), _ptr(workspace), workspace.numel())
+    return weight_out, position_out, kept_len
 
 
 def tv_validate_inputs(page_table, kv_len, parent, *, P: int, num_pages: int, num_nodes=None,

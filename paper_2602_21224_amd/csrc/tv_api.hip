@@ -345,6 +345,113 @@ int kv_compact_accepted(const uint16_t *k_tree, const uint16_t *v_tree, uint16_t
     return e == hipSuccess ? TV_OK : TV_ERR_HIP;
 }
 
+size_t tv_shared_attention_workspace_size(int B, int N, int Hq, int Hkv, int D, int groups) {
+    if (!attn_shape_ok(B, N, Hq, Hkv, D) || B > tv::kMaxBatchShared || groups < 0 ||
+        groups > tv::kMaxGroups)
+        return 0;
+    return 256;
+}
+
+int tree_verify_attention_shared(
+    const uint16_t *q, const uint16_t *k_tree, const uint16_t *v_tree, const uint16_t *k_cache,
+    const uint16_t *v_cache, const int32_t *page_table, const int32_t *kv_len,
+    const int32_t *parent, const int32_t *num_nodes, const int32_t *group_start,
+    const int32_t *shared_len, int groups, int B, int N, int Hq, int Hkv, int D, int P,
+    int max_pages, int num_pages, int max_kv_len, float scale, uint16_t *out, float *lse,
+    void *workspace, size_t workspace_bytes, hipStream_t stream) {
+    if (!attn_shape_ok(B, N, Hq, Hkv, D) || B > tv::kMaxBatchShared) return TV_ERR_SHAPE;
+    if (!pow2(P) || P > 256 || max_pages < 1 || num_pages < 1 || max_kv_len < 0 ||
+        (long)max_pages * P > INT32_MAX || groups < 0 || groups > tv::kMaxGroups)
+        return TV_ERR_SHAPE;
+    if (B == 0) return TV_OK;
+    if (!q || !k_tree || !v_tree || !k_cache || !v_cache || !page_table || !kv_len || !parent ||
+        !out || !workspace || (groups > 0 && (!group_start || !shared_len)))
+        return TV_ERR_NULL;
+    if (!aligned16(q) || !aligned16(k_tree) || !aligned16(v_tree) || !aligned16(k_cache) ||
+        !aligned16(v_cache) || !aligned16(out) || !aligned16(workspace))
+        return TV_ERR_ALIGN;
+    if (workspace_bytes < tv_shared_attention_workspace_size(B, N, Hq, Hkv, D, groups))
+        return TV_ERR_WORKSPACE;
+    if (!device_ok()) return TV_ERR_DEVICE;
+    tv::AttnParams p{};
+    p.q = q; p.k_tree = k_tree; p.v_tree = v_tree; p.k_cache = k_cache; p.v_cache = v_cache;
+    p.page_table = page_table; p.kv_len = kv_len; p.parent = parent; p.num_nodes = num_nodes;
+    p.out = out; p.lse = lse;
+    p.B = B; p.N = N; p.Hq = Hq; p.Hkv = Hkv; p.G = Hq / Hkv;
+    p.P = P; p.p_shift = __builtin_ctz((unsigned)P);
+    p.max_pages = max_pages; p.num_pages = num_pages;
+    p.scale = scale > 0.f ? scale : 1.0f / sqrtf((float)D);
+    p.scale_log2 = p.scale * 1.4426950408889634f;
+    return tv::launch_shared_attention(p, D, stream) == hipSuccess ? TV_OK : TV_ERR_HIP;
+}
+
+int kv_accumulate_weights(const uint16_t *q, const float *lse, const uint16_t *k_cache,
+                          const int32_t *page_table, const int32_t *kv_len,
+                          const int32_t *accept_idx, const int32_t *accept_len,
+                          const int32_t *seen, const int32_t *fixed_len, const float *weight,
+                          int B, int N, int Hq, int Hkv, int D, int P, int max_pages,
+                          int num_pages, int max_kv_len, float scale, float *weight_out,
+                          int32_t *position, hipStream_t stream) {
+    if (B < 0 || B > 65535 || Hkv > 65535 || !attn_shape_ok(1, N, Hq, Hkv, D) || !pow2(P) ||
+        P > 256 || max_pages < 1 || num_pages < 1 || max_kv_len < 0 ||
+        (long)max_pages * P > (1l << 24))
+        return TV_ERR_SHAPE;
+    if (B == 0) return TV_OK;
+    if (!q || !lse || !k_cache || !page_table || !kv_len || !accept_idx || !accept_len || !seen ||
+        !weight || !weight_out || !position)
+        return TV_ERR_NULL;
+    if (!aligned16(q) || !aligned16(k_cache)) return TV_ERR_ALIGN;
+    if (!device_ok()) return TV_ERR_DEVICE;
+    tv::WeightParams p;
+    p.q = q; p.k_cache = k_cache; p.lse = lse; p.weight = weight;
+    p.page_table = page_table; p.kv_len = kv_len; p.accept_idx = accept_idx;
+    p.accept_len = accept_len; p.seen = seen; p.fixed_len = fixed_len;
+    p.weight_out = weight_out; p.position = position;
+    p.B = B; p.N = N; p.Hq = Hq; p.Hkv = Hkv;
+    p.p_shift = __builtin_ctz((unsigned)P); p.max_pages = max_pages; p.num_pages = num_pages;
+    const long cap = (long)max_pages * P, hint = (long)max_kv_len + N;
+    p.max_keys = (int)(hint < cap ? hint : cap);
+    p.scale = scale > 0.f ? scale : 1.0f / sqrtf((float)D);
+    return tv::launch_accumulate_weights(p, D, stream) == hipSuccess ? TV_OK : TV_ERR_HIP;
+}
+
+static bool evict_shape_ok(int B, int Hkv, int max_pages, int P) {
+    return B >= 0 && B <= 65535 && Hkv >= 1 && Hkv <= 65535 && max_pages >= 1 && pow2(P) &&
+           P <= 256 && (long)max_pages * P <= (1l << 24);
+}
+
+size_t tv_evict_workspace_size(int B, int Hkv, int max_pages, int P) {
+    if (!evict_shape_ok(B, Hkv, max_pages, P)) return 0;
+    return round_up((size_t)B * Hkv * max_pages * P * sizeof(int32_t), 256) + 256;
+}
+
+int kv_evict(const float *weight, const int32_t *position, uint16_t *k_cache, uint16_t *v_cache,
+             const int32_t *page_table, const int32_t *kv_len, const int32_t *seen,
+             const int32_t *fixed_len, int B, int Hkv, int D, int P, int max_pages, int num_pages,
+             int max_kv_len, int budget, int recent, float *weight_out, int32_t *position_out,
+             int32_t *kept_len, void *workspace, size_t workspace_bytes, hipStream_t stream) {
+    if (!evict_shape_ok(B, Hkv, max_pages, P) || D < 8 || D % 8 != 0 || D > 1024 ||
+        num_pages < 1 || max_kv_len < 0 || budget < 0 || recent < 0)
+        return TV_ERR_SHAPE;
+    if (B == 0) return TV_OK;
+    if (!weight || !position || !k_cache || !v_cache || !page_table || !kv_len || !seen ||
+        !weight_out || !position_out || !kept_len || !workspace)
+        return TV_ERR_NULL;
+    if (!aligned16(k_cache) || !aligned16(v_cache) || !aligned16(workspace)) return TV_ERR_ALIGN;
+    if (workspace_bytes < tv_evict_workspace_size(B, Hkv, max_pages, P)) return TV_ERR_WORKSPACE;
+    if (!device_ok()) return TV_ERR_DEVICE;
+    tv::EvictParams p;
+    p.weight = weight; p.position = position; p.page_table = page_table; p.kv_len = kv_len;
+    p.seen = seen; p.fixed_len = fixed_len; p.k_cache = k_cache; p.v_cache = v_cache;
+    p.weight_out = weight_out; p.position_out = position_out; p.kept_len = kept_len;
+    p.moves = static_cast<int32_t *>(workspace);
+    p.B = B; p.Hkv = Hkv; p.D = D; p.p_shift = __builtin_ctz((unsigned)P);
+    p.max_pages = max_pages; p.num_pages = num_pages; p.budget = budget; p.recent = recent;
+    const long cap = (long)max_pages * P;
+    p.max_keys = (int)(max_kv_len < cap ? max_kv_len : cap);
+    return tv::launch_evict(p, stream) == hipSuccess ? TV_OK : TV_ERR_HIP;
+}
+
 int tv_validate_inputs(const int32_t *page_table, const int32_t *kv_len, const int32_t *parent,
                        const int32_t *num_nodes, int B, int N, int P, int max_pages,
                        int num_pages, int32_t *status_word, hipStream_t stream) {

@@ -26,6 +26,8 @@ constexpr int kKeyTile = 64;         // keys per attention tile (two 32-key MFMA
 constexpr int kRowsPerWave = 32;     // query rows per wave (MFMA N dimension)
 constexpr int kMaxNodes = 256;
 constexpr int kMaxBatchAttn = 1024;
+constexpr int kMaxBatchShared = 512; // shared-prefix attention: the LDS tables of sequences and groups
+constexpr int kMaxGroups = 256;
 constexpr int kTbMaxK = 16;          // tree builder: largest branch number
 constexpr int kTbMaxSteps = 16;      // tree builder: most speculative steps
 
@@ -80,6 +82,32 @@ struct AttnParams {
     float scale_log2;            // softmax scale * log2(e)
     float scale;                 // softmax scale
     int whole_units;             // every workgroup takes one unit whole (nothing to merge)
+};
+
+// Launch parameters of the accumulated attention weights (all sizes in elements).
+struct WeightParams {
+    const uint16_t *q, *k_cache;
+    const float *lse, *weight;
+    const int32_t *page_table, *kv_len, *accept_idx, *accept_len, *seen;
+    const int32_t *fixed_len;    // [B] or null (0)
+    float *weight_out;
+    int32_t *position;
+    int B, N, Hq, Hkv, p_shift, max_pages, num_pages;
+    int max_keys;                // host-side bound of kv_len + path rows (sizes the launch only)
+    float scale;
+};
+
+// Launch parameters of the eviction.
+struct EvictParams {
+    const float *weight;
+    const int32_t *position, *page_table, *kv_len, *seen;
+    const int32_t *fixed_len;    // [B] or null (0)
+    uint16_t *k_cache, *v_cache;
+    float *weight_out;
+    int32_t *position_out, *kept_len;
+    int32_t *moves;              // [B, Hkv, T]: per head T / 2 destinations, then T / 2 sources
+    int B, Hkv, D, p_shift, max_pages, num_pages, budget, recent;
+    int max_keys;                // host-side bound of kv_len (sizes the launch only)
 };
 
 // Workgroup -> logical index remap: the hardware hands consecutive workgroup
@@ -143,6 +171,9 @@ hipError_t launch_kv_compact(const uint16_t *k_tree, const uint16_t *v_tree, uin
                              uint16_t *v_cache, const int32_t *page_table, const int32_t *kv_len,
                              const int32_t *accept_idx, const int32_t *accept_len, int B, int N,
                              int Hkv, int D, int P, int max_pages, int num_pages, hipStream_t s);
+hipError_t launch_shared_attention(const AttnParams &p, int head_dim, hipStream_t s);
+hipError_t launch_accumulate_weights(const WeightParams &p, int head_dim, hipStream_t s);
+hipError_t launch_evict(const EvictParams &p, hipStream_t s);
 hipError_t launch_validate(const int32_t *page_table, const int32_t *kv_len,
                            const int32_t *parent, const int32_t *num_nodes, int B, int N, int P,
                            int max_pages, int num_pages, int32_t *status_word, hipStream_t s);
