@@ -48,6 +48,24 @@
 //     lane follows its node's parent links through cross-lane shuffles, larger
 //     trees use pointer doubling in LDS. A masked score is replaced by -inf
 //     (selected, never added).
+//
+// Batches whose sequences share a prefix (the SHARED instances)
+//   * The keys of a group's shared prefix are units of their own, over the
+//     query rows of all its sequences at once: rows of a group are its
+//     sequences' real nodes one after another, in blocks of 256 as above, so a
+//     shared K/V tile is read once per row block of the group instead of once
+//     per row block of every sequence. What each sequence has behind the shared
+//     tiles (its own prefix and its tree) are units as before. Both kinds are
+//     laid end to end and shared out together.
+//   * How many keys are taken together is the kernel's choice: whole tiles, at
+//     most what the shortest sequence of the group has, so shared tiles need no
+//     mask and the sequences' own tiles start at a tile. Results do not depend
+//     on it beyond rounding.
+//   * Every row of such a group has two results to be joined, one per kind. A
+//     unit that one workgroup covers leaves a whole normalised row (shared: in
+//     the workspace, own: in out) and its log-sum-exp, a split unit leaves pieces
+//     as above and a record of the workgroups that hold them; a second kernel
+//     joins them row by row.
 #include "tv_internal.h"
 
 namespace tv {
@@ -126,6 +144,16 @@ __shared__ int g_pages[kPageCache];
 __shared__ int g_cum[kMaxBatchAttn + 1];
 __shared__ int g_len[kMaxBatchAttn];     // clamped prefix length per sequence
 __shared__ unsigned short g_nn[kMaxBatchAttn];   // node count per sequence
+
+// The same for batches that share prefixes. "Virtual sequence" v < groups is the
+// shared prefix of group v, groups + b what sequence b has of its own.
+__shared__ int g_vcum[kMaxGroups + kMaxBatchShared + 1];
+__shared__ int g_slen[kMaxBatchShared];          // clamped prefix length per sequence
+__shared__ int g_ncum[kMaxBatchShared + 1];      // real nodes of the sequences before b
+__shared__ int g_gtiles[kMaxGroups];             // tiles taken together (first: shortest prefix of the group)
+__shared__ int g_first[kMaxGroups], g_last[kMaxGroups];   // first and last sequence that has nodes
+__shared__ unsigned short g_gstart[kMaxGroups + 1];
+__shared__ unsigned short g_group[kMaxBatchShared];       // group of a sequence, or kMaxGroups
 
 __device__ __forceinline__ unsigned lds_addr(const void *p) {
     return (unsigned)(size_t)(const LDS_AS void *)p;
@@ -221,6 +249,122 @@ __device__ void build_cumulative(const AttnParams &p) {
             carry += __shfl(x, kWave - 1);
         }
         if (lane == 0) g_cum[p.B] = carry;
+    }
+    __syncthreads();
+}
+
+// Inclusive prefix maximum or sum over a wave.
+__device__ __forceinline__ int wave_scan_max(int x, int lane) {
+    #pragma unroll
+    for (int off = 1; off < kWave; off <<= 1) {
+        const int y = __shfl_up(x, off);
+        if (lane >= off) x = max(x, y);
+    }
+    return x;
+}
+__device__ __forceinline__ int wave_scan_sum(int x, int lane) {
+    #pragma unroll
+    for (int off = 1; off < kWave; off <<= 1) {
+        const int y = __shfl_up(x, off);
+        if (lane >= off) x += y;
+    }
+    return x;
+}
+
+// Query rows per KV head of group s: those of its sequences' real nodes.
+__device__ __forceinline__ int group_rows(int s, const AttnParams &p) {
+    return (g_ncum[g_gstart[s + 1]] - g_ncum[g_gstart[s]]) * p.G;
+}
+
+// Prefix tiles of sequence b that its group takes together.
+__device__ __forceinline__ int shared_tiles_of(int b) {
+    const int s = g_group[b];
+    return s < kMaxGroups ? g_gtiles[s] : 0;
+}
+
+// The tables of a batch with shared prefixes, by all threads; w = 0 leaves what
+// the joining kernel needs of them in the workspace.
+template <int NT>
+__device__ void build_shared_tables(const AttnParams &p, int w) {
+    const int tid = threadIdx.x, lane = tid & (kWave - 1);
+    if (tid < kWave) {
+        int top = 0;                     // a start counts as the largest before it
+        for (int s0 = 0; s0 <= p.groups && p.groups > 0; s0 += kWave) {
+            const int s = s0 + lane;
+            const int x = s <= p.groups ? min(max(p.group_start[s], 0), p.B) : 0;
+            const int y = max(top, wave_scan_max(x, lane));
+            if (s <= p.groups) g_gstart[s] = (unsigned short)y;
+            top = __shfl(y, kWave - 1);
+        }
+    } else if (tid < 2 * kWave) {
+        int carry = 0;
+        for (int b0 = 0; b0 < p.B; b0 += kWave) {
+            const int b = b0 + lane;
+            const int n = b < p.B ? nodes_of(b, p) : 0;
+            const int x = wave_scan_sum(n, lane);
+            if (b < p.B) {
+                g_ncum[b] = carry + x - n;
+                g_slen[b] = clamp_len(p.kv_len[b], p);
+            }
+            carry += __shfl(x, kWave - 1);
+        }
+        if (lane == 0) g_ncum[p.B] = carry;
+    }
+    for (int s = tid; s < p.groups; s += NT) {
+        g_gtiles[s] = 0x7FFFFFFF;
+        g_first[s] = 0x7FFFFFFF;
+        g_last[s] = -1;
+    }
+    __syncthreads();
+    for (int b = tid; b < p.B; b += NT) {
+        int s = kMaxGroups;
+        if (p.groups > 0 && b >= g_gstart[0] && b < g_gstart[p.groups]) {
+            int lo = 0, hi = p.groups - 1;           // the last group that starts at or before b
+            while (lo < hi) {
+                const int mid = (lo + hi + 1) >> 1;
+                if (g_gstart[mid] <= b) lo = mid; else hi = mid - 1;
+            }
+            s = lo;
+        }
+        g_group[b] = (unsigned short)s;
+        if (s < kMaxGroups && g_ncum[b + 1] > g_ncum[b]) {
+            atomicMin(&g_gtiles[s], g_slen[b]);
+            atomicMin(&g_first[s], b);
+            atomicMax(&g_last[s], b);
+        }
+    }
+    __syncthreads();
+    for (int s = tid; s < p.groups; s += NT)
+        g_gtiles[s] = g_last[s] > g_first[s] ? max(min(g_gtiles[s], p.shared_len[s]), 0) / KT : 0;
+    __syncthreads();
+    if (tid < kWave) {
+        int carry = 0;
+        const int nv = p.groups + p.B;
+        for (int v0 = 0; v0 < nv; v0 += kWave) {
+            const int v = v0 + lane;
+            int t = 0;
+            if (v < p.groups) {
+                if (g_gtiles[v] > 0)
+                    t = p.Hkv * row_blocks_of(group_rows(v, p), p) * (p.setup_tiles + g_gtiles[v]);
+            } else if (v < nv) {
+                const int b = v - p.groups;
+                t = p.Hkv * tiles_per_head((g_slen[b] + KT - 1) / KT - shared_tiles_of(b),
+                                           (g_ncum[b + 1] - g_ncum[b]) * p.G, p);
+            }
+            const int x = wave_scan_sum(t, lane);
+            if (v < nv) g_vcum[v] = carry + x - t;
+            carry += __shfl(x, kWave - 1);
+        }
+        if (lane == 0) g_vcum[nv] = carry;
+    } else if (w == 0) {
+        for (int b = tid - kWave; b < p.B; b += NT - kWave) {
+            // nodes before b in its group, the group's first row block (see
+            // shared_unit), shared tiles, node count
+            const int s = g_group[b], n0 = s < kMaxGroups ? g_ncum[g_gstart[s]] : 0;
+            reinterpret_cast<i32x4 *>(p.ws_seq)[b] =
+                i32x4{g_ncum[b] - n0, s < kMaxGroups ? n0 * p.G / p.rows_per_block + s : 0, shared_tiles_of(b),
+                      g_ncum[b + 1] - g_ncum[b]};
+        }
     }
     __syncthreads();
 }
@@ -854,8 +998,34 @@ __device__ __forceinline__ void narrow_tile(NarrowState<D> &st, unsigned kbase, 
     }
 }
 
-template <int D, int NW, bool SMALL, bool NARROW, bool WHOLE>
+// Row (node of all sequences, per head) of node `ord` of group s.
+__device__ __forceinline__ size_t group_node(int s, int ord, const AttnParams &p) {
+    int lo = g_gstart[s], hi = g_gstart[s + 1] - 1;
+    const int o = ord + g_ncum[lo];
+    while (lo < hi) {                    // the last sequence whose nodes start at or before o
+        const int mid = (lo + hi + 1) >> 1;
+        if (g_ncum[mid] <= o) lo = mid; else hi = mid - 1;
+    }
+    return (size_t)lo * p.N + (o - g_ncum[lo]);
+}
+
+// Numbers of the units in ws_unit: the sequences' own ones, then the shared ones.
+// A group of R rows behind X rows of groups before it has at most
+// floor((X + R) / block) - floor(X / block) + 1 row blocks, so with one more per
+// group before it the blocks of all groups get numbers of their own.
+__device__ __forceinline__ int own_unit(int b, int g, int rb, const AttnParams &p) {
+    return (b * p.Hkv + g) * row_blocks_of(p.N * p.G, p) + rb;
+}
+__device__ __forceinline__ int shared_unit_of(int block, int g, const AttnParams &p) {
+    return p.B * p.Hkv * row_blocks_of(p.N * p.G, p) + block * p.Hkv + g;
+}
+__device__ __forceinline__ int shared_unit(int s, int g, int rb, const AttnParams &p) {
+    return shared_unit_of(g_ncum[g_gstart[s]] * p.G / p.rows_per_block + s + rb, g, p);
+}
+
+template <int D, int NW, bool SMALL, bool NARROW, bool WHOLE, bool SHARED = false>
 __global__ __launch_bounds__(NW * kWave) void tree_attention_kernel(AttnParams p) {
+    static_assert(!SHARED || (!NARROW && !WHOLE), "shared prefixes: wide units, split");
     using Gm = Geo<D>;
     using Issue = TileIssue<D, NW, SMALL>;
     constexpr int NT = NW * kWave;
@@ -870,9 +1040,10 @@ __global__ __launch_bounds__(NW * kWave) void tree_attention_kernel(AttnParams p
     const int col = lane & 31;
     const int w = xcd_contiguous_id(blockIdx.x, p.num_wg);
 
-    build_cumulative<NT>(p);
+    if constexpr (SHARED) build_shared_tables<NT>(p, w);
+    else build_cumulative<NT>(p);
 
-    const int total = g_cum[p.B];
+    const int total = SHARED ? g_vcum[p.groups + p.B] : g_cum[p.B];
     // Workgroup u < nw takes virtual tiles [share_start(u), share_start(u + 1)):
     // shares differ by at most one tile and none is empty (nw <= total), so the
     // pieces of a split unit sit in consecutive workgroups. Workgroups past nw
@@ -904,36 +1075,70 @@ __global__ __launch_bounds__(NW * kWave) void tree_attention_kernel(AttnParams p
 
     int pos = start;
     int anc_b = -1;                 // sequence whose ancestor sets are in g_anc
-    if (start >= end && tid == 0) p.ws_desc[w * 4] = -1;
+    if (!SHARED && start >= end && tid == 0) p.ws_desc[w * 4] = -1;
     while (pos < end) {
         // ---- locate the unit holding tile `pos`
-        int lo = 0, hi = p.B - 1;
-        while (lo < hi) {
-            const int mid = (lo + hi + 1) >> 1;
-            if (g_cum[mid] <= pos) lo = mid; else hi = mid - 1;
-        }
-        const int b = lo;
-        const int L = g_len[b];
-        const int nodes = g_nn[b];
-        const int rows_b = nodes * p.G;                 // this sequence's query rows per KV head
-        const int ntp = (L + KT - 1) / KT;
+        int b, L, nodes, rows_b, ntp;   // rows_b: the unit's sequence's query rows per KV head
+        int ts = 0;                     // the unit's first tile (behind the tiles taken together)
+        int sg = -1;                    // shared unit: its group; b is then the sequence whose pages are read
         const int C = p.setup_tiles;
-        const int per_g = tiles_per_head(ntp, rows_b, p);
-        int off = pos - g_cum[b];
-        const int g = off / per_g;
-        off -= g * per_g;
-        int rb = 0;
-        int ulen = ntp + tree_tiles_of_block(0, rows_b, p);     // real tiles of the unit
-        while (off >= C + ulen) {
-            off -= C + ulen;
-            ++rb;
-            ulen = ntp + tree_tiles_of_block(rb, rows_b, p);
+        int off, g, rb = 0, ulen;       // ulen: real tiles of the unit
+        if constexpr (SHARED) {
+            int lo = 0, hi = p.groups + p.B - 1;
+            while (lo < hi) {
+                const int mid = (lo + hi + 1) >> 1;
+                if (g_vcum[mid] <= pos) lo = mid; else hi = mid - 1;
+            }
+            off = pos - g_vcum[lo];
+            if (lo < p.groups) {
+                sg = lo;
+                b = g_first[sg];
+                ntp = g_gtiles[sg];
+                L = ntp * KT;
+                nodes = 1;              // of sequence b: it has one at least
+                rows_b = group_rows(sg, p);
+                ulen = ntp;
+                const int u = off / (C + ulen), rbs = row_blocks_of(rows_b, p);
+                off -= u * (C + ulen);
+                g = u / rbs;
+                rb = u - g * rbs;
+            } else {
+                b = lo - p.groups;
+                L = g_slen[b];
+                nodes = g_ncum[b + 1] - g_ncum[b];
+                rows_b = nodes * p.G;
+                ntp = (L + KT - 1) / KT;
+                ts = shared_tiles_of(b);
+            }
+        } else {
+            int lo = 0, hi = p.B - 1;
+            while (lo < hi) {
+                const int mid = (lo + hi + 1) >> 1;
+                if (g_cum[mid] <= pos) lo = mid; else hi = mid - 1;
+            }
+            b = lo;
+            L = g_len[b];
+            nodes = g_nn[b];
+            rows_b = nodes * p.G;
+            ntp = (L + KT - 1) / KT;
+            off = pos - g_cum[b];
+        }
+        if (!SHARED || sg < 0) {
+            const int per_g = tiles_per_head(ntp - ts, rows_b, p);
+            g = off / per_g;
+            off -= g * per_g;
+            ulen = ntp - ts + tree_tiles_of_block(0, rows_b, p);
+            while (off >= C + ulen) {
+                off -= C + ulen;
+                ++rb;
+                ulen = ntp - ts + tree_tiles_of_block(rb, rows_b, p);
+            }
         }
         // this share covers virtual tiles [off, v_end) of the unit; real tile
         // r is virtual tile C + r
         const int v_end = min(C + ulen, off + (end - pos));
         const int unit_real_start = pos - off + C;    // share coordinate of real tile 0
-        const int t0 = max(off - C, 0);
+        const int t0 = ts + max(off - C, 0);
         // Page ids of the first four tiles (scalar loads): for narrow units first
         // of all, so that their latency overlaps the rest of the set-up; for the
         // others after the parent links (holding them that long costs the
@@ -943,7 +1148,7 @@ __global__ __launch_bounds__(NW * kWave) void tree_attention_kernel(AttnParams p
             #pragma unroll
             for (int i = 0; i < 4; ++i) ld.fetch_pages(p, b, t0 + i, wave_u, ids[i]);
         }
-        if (pos == start && tid == 0) {
+        if (!SHARED && pos == start && tid == 0) {
             // the merge kernel's entry for this workgroup: the split unit whose
             // last piece is this share's first, if any
             const int wf = share_of(unit_real_start);
@@ -953,9 +1158,9 @@ __global__ __launch_bounds__(NW * kWave) void tree_attention_kernel(AttnParams p
                      : i32x4{-1, 0, 0, 0};
         }
         pos += v_end - off;
-        const int t_end = v_end - C;
+        const int t_end = ts + v_end - C;
         if (t_end <= t0) continue;                    // only set-up tiles of this unit
-        const bool complete = (t0 == 0 && t_end == ulen);
+        const bool complete = (t0 == ts && t_end == ts + ulen);
 
         // Parent links for the ancestor sets (trees of up to 64 nodes), loaded
         // before any other load of the piece so that waiting for them never
@@ -978,8 +1183,15 @@ __global__ __launch_bounds__(NW * kWave) void tree_attention_kernel(AttnParams p
         const int row = rb * p.rows_per_block + wave_u * kRowsPerWave + col;
         const bool row_ok = row < rows_b;
         const int qrow = row_ok ? row : rb * p.rows_per_block;
-        const int node = qrow / p.G;
+        int node = qrow / p.G;
         const int hq = g * p.G + qrow % p.G;
+        size_t qnode = (size_t)b * p.N + node;          // row of q, out and lse (per head)
+        if constexpr (SHARED) {
+            if (sg >= 0) {
+                qnode = group_node(sg, node, p);
+                node = 0;
+            }
+        }
         WaveState<D> st;
         NarrowState<D> ns;
         // narrow units: lane l holds row l % 16 (rows past the unit's last load
@@ -987,7 +1199,7 @@ __global__ __launch_bounds__(NW * kWave) void tree_attention_kernel(AttnParams p
         const int nrow = NARROW ? min(lane & 15, rows_b - 1) : 0;
         const int nnode = nrow / p.G;
         if constexpr (!NARROW) {
-            const uint16_t *qp = p.q + (((size_t)b * p.N + node) * p.Hq + hq) * D + half * 8;
+            const uint16_t *qp = p.q + (qnode * p.Hq + hq) * D + half * 8;
             #pragma unroll
             for (int ks = 0; ks < NKS; ++ks)
                 st.qf[ks] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const u16x8 *>(qp + ks * 16));
@@ -1226,6 +1438,13 @@ __global__ __launch_bounds__(NW * kWave) void tree_attention_kernel(AttnParams p
         // sum) pair (fp32): slot 0 holds the piece that continues a unit from
         // before this share, slot 1 the one that starts inside it.
         const int slot = w * 2 + (unit_real_start <= start ? 0 : 1);
+        if (SHARED && tid == 0) {
+            // where the joining kernel finds the unit: the slot of its first piece
+            // (-1: a whole unit, its rows are in out or ws_so) and the workgroup of its last
+            int32_t *rec = p.ws_unit + 2 * (sg >= 0 ? shared_unit(sg, g, rb, p) : own_unit(b, g, rb, p));
+            if (t0 == ts) rec[0] = complete ? -1 : slot;
+            if (t_end == ts + ulen) rec[1] = w;
+        }
         if constexpr (!NARROW) {
             const float l_tot = halves_sum(st.l_run);
             const float inv = l_tot > 0.f ? 1.f / l_tot : 0.f;
@@ -1251,7 +1470,9 @@ __global__ __launch_bounds__(NW * kWave) void tree_attention_kernel(AttnParams p
                     const int ur = rb * p.rows_per_block + rl;
                     if (ur < rows_b) {
                         const int nd = ur / p.G, h = g * p.G + ur % p.G;
-                        *reinterpret_cast<u32x4 *>(p.out + (((size_t)b * p.N + nd) * p.Hq + h) * D + ch * 8) = v;
+                        const size_t on = SHARED && sg >= 0 ? group_node(sg, nd, p) : (size_t)b * p.N + nd;
+                        uint16_t *o = SHARED && sg >= 0 ? p.ws_so : p.out;
+                        *reinterpret_cast<u32x4 *>(o + (on * p.Hq + h) * D + ch * 8) = v;
                     }
                 } else {
                     *reinterpret_cast<u32x4 *>(p.ws_o + ((size_t)slot * p.rows_per_block + rl) * D + ch * 8) = v;
@@ -1259,8 +1480,11 @@ __global__ __launch_bounds__(NW * kWave) void tree_attention_kernel(AttnParams p
             }
             if (half == 0) {
                 if (complete) {
-                    if (row_ok && p.lse)
-                        p.lse[((size_t)b * p.N + node) * p.Hq + hq] =
+                    if (SHARED && row_ok)       // base 2; ws_lse2: the shared part's, then the own part's
+                        p.ws_lse2[(sg >= 0 ? 0 : (size_t)p.B * p.N * p.Hq) + qnode * p.Hq + hq] =
+                            st.m_run * p.scale_log2 + __builtin_amdgcn_logf(l_tot);
+                    if (row_ok && p.lse && !(SHARED && sg >= 0))
+                        p.lse[qnode * p.Hq + hq] =
                             st.m_run * p.scale + __builtin_amdgcn_logf(l_tot) * kLn2;
                 } else {
                     const int rloc = wave_u * kRowsPerWave + col;
@@ -1337,7 +1561,7 @@ __global__ __launch_bounds__(NW * kWave) void tree_attention_kernel(AttnParams p
         const int chunks = p.Hq * D / 8;             // 16-byte chunks of one node's output
         for (int idx = w; idx < p.B * p.N; idx += p.num_wg) {
             const int b = idx / p.N, i = idx - b * p.N;
-            if (i < g_nn[b]) continue;
+            if (i < (SHARED ? g_ncum[b + 1] - g_ncum[b] : g_nn[b])) continue;
             u16x8 *op = reinterpret_cast<u16x8 *>(p.out + ((size_t)b * p.N + i) * p.Hq * D);
             for (int c = tid; c < chunks; c += NT) op[c] = u16x8{0, 0, 0, 0, 0, 0, 0, 0};
             if (p.lse)
@@ -1400,6 +1624,65 @@ __global__ __launch_bounds__(256) void tree_attention_merge_kernel(AttnParams p,
         p.lse[((size_t)b * p.N + node) * p.Hq + hq] = (M + __builtin_amdgcn_logf(den)) * kLn2;
 }
 
+// Join the results of every row of a batch with shared prefixes: those of its
+// group's shared keys, if any, and those of its sequence's own keys, each one
+// row or the pieces of a split unit. One thread per (row, 8 head-dim lanes), in
+// the order of `out`; pieces are combined in workgroup order with an online
+// log-sum-exp rescale. Rows with one whole result have it in `out` already.
+template <int D>
+__global__ __launch_bounds__(256) void shared_join_kernel(AttnParams p) {
+    constexpr int D8 = D / 8;
+    const size_t row = (size_t)blockIdx.x * (256 / D8) + threadIdx.x / D8;
+    const int d8 = threadIdx.x % D8;
+    const size_t rows = (size_t)p.B * p.N * p.Hq;
+    if (row >= rows) return;
+    const int h = (int)(row % p.Hq), i = (int)(row / p.Hq % p.N), b = (int)(row / ((size_t)p.Hq * p.N));
+    const i32x4 sq = reinterpret_cast<const i32x4 *>(p.ws_seq)[b];
+    if (i >= sq[3]) return;                         // padding: written by the main kernel
+    const int g = h / p.G;
+    const int own_row = i * p.G + h % p.G;
+    const int group_row = sq[0] * p.G + own_row;
+    const int *own = p.ws_unit + 2 * own_unit(b, g, own_row / p.rows_per_block, p);
+    const int *shr = p.ws_unit + 2 * shared_unit_of(sq[1] + group_row / p.rows_per_block, g, p);
+    const bool shared = sq[2] > 0;
+    const int own_first = own[0], own_last = own[1];
+    if (!shared && own_first < 0) return;
+
+    float M = kNegInf, den = 0.f;
+    float acc[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    auto add = [&](const uint16_t *o, float m, float l) {
+        const bf16x8 v = *reinterpret_cast<const bf16x8 *>(o + d8 * 8);
+        const float Mn = fmaxf(M, m);
+        const float sc = (M == kNegInf) ? 0.f : __builtin_amdgcn_exp2f(M - Mn);
+        const float wt = (m == kNegInf) ? 0.f : __builtin_amdgcn_exp2f(m - Mn) * l;
+        den = den * sc + wt;
+        #pragma unroll
+        for (int e = 0; e < 8; ++e) acc[e] = acc[e] * sc + wt * (float)v[e];
+        M = Mn;
+    };
+    auto add_unit = [&](int first, int last, int rl, const uint16_t *whole, const float *lse2) {
+        if (first < 0) {
+            add(whole + row * D, lse2[row], 1.f);
+            return;
+        }
+        #pragma unroll 4
+        for (int u = first >> 1; u <= last; ++u) {
+            // the first piece may sit in slot 1 of its workgroup; later ones start a share
+            const size_t r = (size_t)(u == (first >> 1) ? first : u * 2) * p.rows_per_block + rl;
+            const f32x2 ml = *reinterpret_cast<const f32x2 *>(p.ws_ml + r * 2);
+            add(p.ws_o + r * D, ml[0], ml[1]);
+        }
+    };
+    if (shared) add_unit(shr[0], shr[1], group_row % p.rows_per_block, p.ws_so, p.ws_lse2);
+    add_unit(own_first, own_last, own_row % p.rows_per_block, p.out, p.ws_lse2 + rows);
+    const float inv = den > 0.f ? 1.f / den : 0.f;
+    bf16x8 o;
+    #pragma unroll
+    for (int e = 0; e < 8; ++e) o[e] = (__bf16)(acc[e] * inv);
+    *reinterpret_cast<bf16x8 *>(p.out + row * D + d8 * 8) = o;
+    if (p.lse && d8 == 0) p.lse[row] = (M + __builtin_amdgcn_logf(den)) * kLn2;
+}
+
 // Units taken whole have instances of their own, so that the split ones keep their
 // code: with the choice inside the kernel it came out up to 0.8 % slower (45 nodes of
 // head size 64 over 300-2500 keys 21.1 -> 21.3 us).
@@ -1441,6 +1724,21 @@ hipError_t launch_d(const AttnParams &p, int waves, hipStream_t s) {
 }
 
 }  // namespace
+
+template <int D>
+hipError_t launch_shared_d(const AttnParams &p, hipStream_t s) {
+    constexpr int NW = 8;
+    const auto kernel = p.small_pages ? tree_attention_kernel<D, NW, true, false, false, true>
+                                      : tree_attention_kernel<D, NW, false, false, false, true>;
+    const hipError_t e = launch_kernel(kernel, dim3(p.num_wg), dim3(NW * kWave), s, p);
+    if (e != hipSuccess) return e;
+    const size_t rows = (size_t)p.B * p.N * p.Hq, per = 256 / (D / 8);
+    return launch_kernel(shared_join_kernel<D>, dim3((unsigned)((rows + per - 1) / per)), dim3(256), s, p);
+}
+
+hipError_t launch_shared_attention(const AttnParams &p, int head_dim, hipStream_t s) {
+    return head_dim == 64 ? launch_shared_d<64>(p, s) : launch_shared_d<128>(p, s);
+}
 
 hipError_t launch_tree_attention(const AttnParams &p, int head_dim, int waves, hipStream_t s) {
     if (head_dim == 64) return launch_d<64>(p, waves, s);

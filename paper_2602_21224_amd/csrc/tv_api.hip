@@ -111,6 +111,42 @@ AttnWorkspace attn_workspace(const AttnShape &s, int D, int max_wg) {
     return w;
 }
 
+// Batches with shared prefixes run workgroups of eight waves throughout: a
+// group's rows are many, and a period of few rows is bound by its tile loads,
+// which eight waves issue as fast as four.
+AttnShape shared_shape(int N, int Hq, int Hkv) {
+    AttnShape s = attn_shape(N, Hq, Hkv);
+    s.waves = 8;
+    s.rows_per_block = s.waves * tv::kRowsPerWave;
+    s.row_blocks = (s.rows + s.rows_per_block - 1) / s.rows_per_block;
+    s.tree_tiles_all = s.row_blocks * ((N + tv::kKeyTile - 1) / tv::kKeyTile);   // at most
+    return s;
+}
+
+// Most row blocks per KV head that the groups' shared units can have together.
+long shared_blocks(const AttnShape &s, int B, int groups) {
+    return ((long)B * s.rows + s.rows_per_block - 1) / s.rows_per_block + groups;
+}
+
+struct SharedWorkspace {
+    AttnWorkspace split;
+    size_t so, lse2, unit, seq, total;       // byte offsets, and the whole
+};
+
+SharedWorkspace shared_workspace(const AttnShape &s, int B, int N, int Hq, int Hkv, int D, int groups,
+                                 int max_wg) {
+    SharedWorkspace w;
+    const size_t rows = (size_t)B * N * Hq;
+    const size_t units = ((size_t)B * s.row_blocks + (size_t)shared_blocks(s, B, groups)) * Hkv;
+    w.split = attn_workspace(s, D, max_wg);
+    w.so = w.split.o_bytes + w.split.ml_bytes;
+    w.lse2 = w.so + round_up(rows * D * sizeof(uint16_t), 256);
+    w.unit = w.lse2 + round_up(rows * 2 * sizeof(float), 256);
+    w.seq = w.unit + round_up(units * 2 * sizeof(int32_t), 256);
+    w.total = w.seq + round_up((size_t)B * 4 * sizeof(int32_t), 256) + 256;
+    return w;
+}
+
 bool attn_shape_ok(int B, int N, int Hq, int Hkv, int D) {
     if (B < 0 || B > tv::kMaxBatchAttn) return false;
     if (N < 1 || N > tv::kMaxNodes) return false;
@@ -349,7 +385,7 @@ size_t tv_shared_attention_workspace_size(int B, int N, int Hq, int Hkv, int D, 
     if (!attn_shape_ok(B, N, Hq, Hkv, D) || B > tv::kMaxBatchShared || groups < 0 ||
         groups > tv::kMaxGroups)
         return 0;
-    return 256;
+    return shared_workspace(shared_shape(N, Hq, Hkv), B, N, Hq, Hkv, D, groups, cu_count() * kWgPerCu).total;
 }
 
 int tree_verify_attention_shared(
@@ -370,9 +406,23 @@ int tree_verify_attention_shared(
     if (!aligned16(q) || !aligned16(k_tree) || !aligned16(v_tree) || !aligned16(k_cache) ||
         !aligned16(v_cache) || !aligned16(out) || !aligned16(workspace))
         return TV_ERR_ALIGN;
-    if (workspace_bytes < tv_shared_attention_workspace_size(B, N, Hq, Hkv, D, groups))
-        return TV_ERR_WORKSPACE;
+    const AttnShape s = shared_shape(N, Hq, Hkv);
+    const int max_wg = cu_count() * kWgPerCu;
+    const SharedWorkspace ws = shared_workspace(s, B, N, Hq, Hkv, D, groups, max_wg);
+    if (workspace_bytes < ws.total) return TV_ERR_WORKSPACE;
+
+    // the (virtual) tile count of the whole launch must fit in int32 for any kv_len
+    const long max_len = (long)max_pages * P;
+    const long blocks = (long)B * s.row_blocks + shared_blocks(s, B, groups);
+    auto tiles = [&](long len) {
+        return Hkv * (blocks * ((len + tv::kKeyTile - 1) / tv::kKeyTile + kSetupTiles) + (long)B * s.tree_tiles_all);
+    };
+    if (tiles(max_len) >= (1l << 30)) return TV_ERR_SHAPE;
     if (!device_ok()) return TV_ERR_DEVICE;
+    long num_wg = tiles(max_kv_len < max_len ? max_kv_len : max_len) / kMinShareTiles;
+    if (num_wg < 1) num_wg = 1;
+    if (num_wg > max_wg) num_wg = max_wg;
+
     tv::AttnParams p{};
     p.q = q; p.k_tree = k_tree; p.v_tree = v_tree; p.k_cache = k_cache; p.v_cache = v_cache;
     p.page_table = page_table; p.kv_len = kv_len; p.parent = parent; p.num_nodes = num_nodes;
@@ -382,6 +432,18 @@ int tree_verify_attention_shared(
     p.max_pages = max_pages; p.num_pages = num_pages;
     p.scale = scale > 0.f ? scale : 1.0f / sqrtf((float)D);
     p.scale_log2 = p.scale * 1.4426950408889634f;
+    char *base = static_cast<char *>(workspace);
+    p.ws_o = reinterpret_cast<uint16_t *>(base);
+    p.ws_ml = reinterpret_cast<float *>(base + ws.split.o_bytes);
+    p.ws_so = reinterpret_cast<uint16_t *>(base + ws.so);
+    p.ws_lse2 = reinterpret_cast<float *>(base + ws.lse2);
+    p.ws_unit = reinterpret_cast<int32_t *>(base + ws.unit);
+    p.ws_seq = reinterpret_cast<int32_t *>(base + ws.seq);
+    p.group_start = group_start; p.shared_len = shared_len; p.groups = groups;
+    p.rows_per_block = s.rows_per_block;
+    p.setup_tiles = kSetupTiles;
+    p.small_pages = P < 1024 / (2 * D) ? 1 : 0;
+    p.num_wg = (int)num_wg;
     return tv::launch_shared_attention(p, D, stream) == hipSuccess ? TV_OK : TV_ERR_HIP;
 }
 

@@ -82,6 +82,13 @@ struct AttnParams {
     float scale_log2;            // softmax scale * log2(e)
     float scale;                 // softmax scale
     int whole_units;             // every workgroup takes one unit whole (nothing to merge)
+    // batches with shared prefixes only
+    const int32_t *group_start, *shared_len;
+    int groups;
+    uint16_t *ws_so;             // [B * N * Hq][D] bf16: rows of whole shared units (normalised)
+    float *ws_lse2;              // [2][B * N * Hq] log-sum-exp (base 2) of whole units: shared, own
+    int32_t *ws_unit;            // [units][2]: slot of the first piece (-1: whole), workgroup of the last
+    int32_t *ws_seq;             // [B][4] per sequence: see build_shared_tables
 };
 
 // Launch parameters of the accumulated attention weights (all sizes in elements).
