@@ -484,7 +484,9 @@ static bool evict_shape_ok(int B, int Hkv, int max_pages, int P) {
 
 size_t tv_evict_workspace_size(int B, int Hkv, int max_pages, int P) {
     if (!evict_shape_ok(B, Hkv, max_pages, P)) return 0;
-    return round_up((size_t)B * Hkv * max_pages * P * sizeof(int32_t), 256) + 256;
+    // the lists of moved slots, and their lengths
+    return round_up((size_t)B * Hkv * max_pages * P * sizeof(int32_t), 256) +
+           round_up((size_t)B * Hkv * sizeof(int32_t), 256) + 256;
 }
 
 int kv_evict(const float *weight, const int32_t *position, uint16_t *k_cache, uint16_t *v_cache,
@@ -502,11 +504,12 @@ int kv_evict(const float *weight, const int32_t *position, uint16_t *k_cache, ui
     if (!aligned16(k_cache) || !aligned16(v_cache) || !aligned16(workspace)) return TV_ERR_ALIGN;
     if (workspace_bytes < tv_evict_workspace_size(B, Hkv, max_pages, P)) return TV_ERR_WORKSPACE;
     if (!device_ok()) return TV_ERR_DEVICE;
-    tv::EvictParams p;
+    tv::EvictParams p{};
     p.weight = weight; p.position = position; p.page_table = page_table; p.kv_len = kv_len;
     p.seen = seen; p.fixed_len = fixed_len; p.k_cache = k_cache; p.v_cache = v_cache;
     p.weight_out = weight_out; p.position_out = position_out; p.kept_len = kept_len;
     p.moves = static_cast<int32_t *>(workspace);
+    p.count = p.moves + round_up((size_t)B * Hkv * max_pages * P * sizeof(int32_t), 256) / sizeof(int32_t);
     p.B = B; p.Hkv = Hkv; p.D = D; p.p_shift = __builtin_ctz((unsigned)P);
     p.max_pages = max_pages; p.num_pages = num_pages; p.budget = budget; p.recent = recent;
     const long cap = (long)max_pages * P;

@@ -113,8 +113,11 @@ struct EvictParams {
     float *weight_out;
     int32_t *position_out, *kept_len;
     int32_t *moves;              // [B, Hkv, T]: per head T / 2 destinations, then T / 2 sources
+    int32_t *count;              // [B, Hkv] moves that are left to the second kernel
     int B, Hkv, D, p_shift, max_pages, num_pages, budget, recent;
     int max_keys;                // host-side bound of kv_len (sizes the launch only)
+    int vector_slots;            // four neighbouring slots can be loaded at once
+    int move_here;               // the selecting workgroup moves the rows itself
 };
 
 // Workgroup -> logical index remap: the hardware hands consecutive workgroup
@@ -180,7 +183,7 @@ hipError_t launch_kv_compact(const uint16_t *k_tree, const uint16_t *v_tree, uin
                              int Hkv, int D, int P, int max_pages, int num_pages, hipStream_t s);
 hipError_t launch_shared_attention(const AttnParams &p, int head_dim, hipStream_t s);
 hipError_t launch_accumulate_weights(const WeightParams &p, int head_dim, hipStream_t s);
-hipError_t launch_evict(const EvictParams &p, hipStream_t s);
+hipError_t launch_evict(EvictParams p, hipStream_t s);
 hipError_t launch_validate(const int32_t *page_table, const int32_t *kv_len,
                            const int32_t *parent, const int32_t *num_nodes, int B, int N, int P,
                            int max_pages, int num_pages, int32_t *status_word, hipStream_t s);
