@@ -12,8 +12,11 @@
 // l % 16 of each of four blocks and head-dim columns 8 (l / 16) + 32 step) and
 // takes the rows 16 at a time on M: lane l then holds the scores of rows
 // 4 (l / 16) + i with its key, and adds their exponentials into one number per
-// key block. Nothing goes through LDS, and waves need no barrier. The sums run
-// over the rows in order and over l / 16 at the end: fixed, without atomics.
+// key block. The page ids of a wave's keys are fetched together and its keys all
+// issued before anything waits for them; meanwhile the workgroup puts what the
+// rows need (place of the query, log-sum-exp, last visible key) into LDS. The
+// sums run over the rows in order and over l / 16 at the end: fixed, without
+// atomics.
 #include "tv_internal.h"
 
 namespace tv {
@@ -21,88 +24,126 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kKeys = 64;                // per wave
+constexpr int kMaxRows = 2048;           // query rows per KV head (path nodes x heads of the group)
 constexpr float kNegInf = -__builtin_huge_valf();
 constexpr float kLog2e = 1.4426950408889634f;
 
 template <int D>
 __global__ __launch_bounds__(kThreads) void accumulate_weights_kernel(WeightParams p) {
     constexpr int NKS = D / 32;          // MFMA steps over the head dim
+    // per path row: its query's offset in 16-byte pieces, its log-sum-exp in base 2, and
+    // the last position it sees (-1: the row adds nothing)
+    __shared__ int s_q[kMaxRows];
+    __shared__ __attribute__((aligned(16))) float s_z[kMaxRows];
+    __shared__ __attribute__((aligned(16))) int s_last[kMaxRows];
     const int b = blockIdx.z, g = blockIdx.y;
     const int lane = threadIdx.x & (kWave - 1), col = lane & 15, quad = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
     const int T = p.max_pages << p.p_shift;
     const int L = min(max(p.kv_len[b], 0), T);
     const int n = min(max(p.accept_len[b], 0), p.N);
     const int fixed = p.fixed_len ? min(max(p.fixed_len[b], 0), L) : 0;
     const int end = min(L + n, T);
+    constexpr int kStep = kThreads / kWave * kKeys;
+    if ((int)blockIdx.x * kStep >= end) return;
     const int G = p.Hq / p.Hkv;
-    const int rows = n * G;
+    const int rows = n * G, padded = (rows + 15) & ~15;
     const size_t base = ((size_t)b * p.Hkv + g) * T;
     const int32_t *table = p.page_table + (size_t)b * p.max_pages;
-    const int32_t *path = p.accept_idx + (size_t)b * p.N;
     const int mask = (1 << p.p_shift) - 1;
     const float c = p.scale * kLog2e;
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
-    const int step = gridDim.x * (kThreads / kWave) * kKeys;
-    for (int t0 = (blockIdx.x * (kThreads / kWave) + wave) * kKeys; t0 < end; t0 += step) {
-        const int mine = t0 + lane;      // the key whose weight this lane writes
-        if (t0 + kKeys <= fixed) {
-            if (p.weight_out != p.weight) p.weight_out[base + mine] = p.weight[base + mine];
-            continue;
-        }
-        // the wave's keys; one without a row in the pool reads the pool's first row and
-        // is not written
-        bf16x8 k[4][NKS];
-        bool ok[4];
+    const uint16_t *qb = p.q + ((size_t)b * p.N * p.Hq + g * G) * D + quad * 8;
+
+    int t0 = blockIdx.x * kStep + wave * kKeys;
+    bf16x8 k[4][NKS];
+    bool ok[4];
+    // the wave's keys; one without a row in the pool reads the pool's first row and is
+    // not written
+    auto load_pages = [&](int (&pg)[4]) {
+        #pragma unroll
+        for (int kb = 0; kb < 4; ++kb) pg[kb] = table[min(t0 + kb * 16 + col, T - 1) >> p.p_shift];
+    };
+    auto load_keys = [&](const int (&pg)[4]) {
         #pragma unroll
         for (int kb = 0; kb < 4; ++kb) {
             const int t = t0 + kb * 16 + col;
-            const int pg = t < end ? table[t >> p.p_shift] : -1;
-            ok[kb] = pg >= 0 && pg < p.num_pages;
-            const size_t slot = ok[kb] ? ((size_t)pg << p.p_shift) + (t & mask) : 0;
+            ok[kb] = t < end && (unsigned)pg[kb] < (unsigned)p.num_pages;
+            const size_t slot = ok[kb] ? ((size_t)pg[kb] << p.p_shift) + (t & mask) : 0;
             const uint16_t *kr = p.k_cache + (slot * p.Hkv + g) * D + quad * 8;
             #pragma unroll
             for (int ks = 0; ks < NKS; ++ks)
                 k[kb][ks] = *reinterpret_cast<const bf16x8 *>(kr + ks * 32);
         }
-        const float old = mine < L ? p.weight[base + mine] : 0.f;
+    };
+    const bool work = t0 < end && t0 + kKeys > fixed;
+    // The first rows' node ids and log-sum-exps are asked for before the keys, which loads
+    // return in order: waiting for them then does not wait for the keys.
+    int pages[4] = {0, 0, 0, 0};
+    if (work) load_pages(pages);
+    int j, nd, at;
+    float z = 0.f;
+    auto ask = [&](int r) {
+        const int x = min(r, rows - 1);
+        j = p.g_inv ? (int)__umulhi((unsigned)x, p.g_inv) : x;
+        nd = p.accept_idx[(size_t)b * p.N + j];
+        at = min(max(nd, 0), p.N - 1) * p.Hq + (x - j * G);
+        z = p.lse[(size_t)b * p.N * p.Hq + g * G + at];
+    };
+    int r = threadIdx.x;
+    if (r < padded) ask(r);
+    if (work) load_keys(pages);
+    while (r < padded) {
+        const bool real = r < rows && (unsigned)nd < (unsigned)p.N && z != kNegInf;
+        s_q[r] = at * (D / 8);
+        s_z[r] = z * kLog2e;
+        s_last[r] = real ? L + j : -1;
+        r += kThreads;
+        if (r < padded) ask(r);
+    }
+    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
 
+    for (bool again = false; t0 < end; t0 += gridDim.x * kStep, again = true) {
+        const int mine = t0 + lane;      // the key whose weight this lane writes
+        if (t0 + kKeys <= fixed) {
+            if (p.weight_out != p.weight) p.weight_out[base + mine] = p.weight[base + mine];
+            continue;
+        }
+        if (again) {
+            load_pages(pages);
+            load_keys(pages);
+        }
+        const float old = mine < L ? p.weight[base + mine] : 0.f;
         float sum[4] = {0.f, 0.f, 0.f, 0.f};
-        for (int r0 = 0; r0 < rows; r0 += 16) {
-            // Q rows on M: lane l loads row l % 16 (a row past the last one, or of a node
-            // out of range, loads node 0's and counts for nothing)
-            const int rq = r0 + col, jq = rq / G;
-            int nq = rq < rows ? path[jq] : 0;
-            if (nq < 0 || nq >= p.N) nq = 0;
-            const uint16_t *qr =
-                p.q + (((size_t)b * p.N + nq) * p.Hq + g * G + (rq - jq * G)) * D + quad * 8;
-            bf16x8 q[NKS];
+        bf16x8 q[2][NKS];
+        auto load_q = [&](int r0, bf16x8 (&x)[NKS]) {
+            const uint16_t *qr = qb + (size_t)s_q[r0 + col] * 8;
             #pragma unroll
-            for (int ks = 0; ks < NKS; ++ks) q[ks] = *reinterpret_cast<const bf16x8 *>(qr + ks * 32);
-            // the rows whose scores this lane gets: their lse, and the last key they see
-            float z[4];
-            int last[4];
-            #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int r = r0 + 4 * quad + i, j = r / G;
-                const int nd = r < rows ? path[j] : -1;
-                const bool real = nd >= 0 && nd < p.N;
-                const float l = real ? p.lse[((size_t)b * p.N + nd) * p.Hq + g * G + (r - j * G)] : kNegInf;
-                z[i] = l * kLog2e;
-                last[i] = l == kNegInf ? -1 : L + j;
-            }
+            for (int ks = 0; ks < NKS; ++ks) x[ks] = *reinterpret_cast<const bf16x8 *>(qr + ks * 32);
+        };
+        auto block = [&](int r0, const bf16x8 (&x)[NKS]) {
+            const f32x4 z = *reinterpret_cast<const f32x4 *>(s_z + r0 + 4 * quad);
+            const i32x4 last = *reinterpret_cast<const i32x4 *>(s_last + r0 + 4 * quad);
             #pragma unroll
             for (int kb = 0; kb < 4; ++kb) {
                 f32x4 s = {0.f, 0.f, 0.f, 0.f};
                 #pragma unroll
                 for (int ks = 0; ks < NKS; ++ks)
-                    s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(q[ks], k[kb][ks], s, 0, 0, 0);
+                    s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x[ks], k[kb][ks], s, 0, 0, 0);
                 const int t = t0 + kb * 16 + col;
                 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i], c, -z[i]));
-                    sum[kb] += t <= last[i] ? x : 0.f;
+                    const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i], c, -z[i]));
+                    sum[kb] += t <= last[i] ? e : 0.f;
                 }
             }
+        };
+        // 16 rows at a time on M (lane l loads row l % 16), the next ones on their way
+        if (padded > 0) load_q(0, q[0]);
+        for (int r0 = 0; r0 < padded; r0 += 32) {
+            if (r0 + 16 < padded) load_q(r0 + 16, q[1]);
+            block(r0, q[0]);
+            if (r0 + 32 < padded) load_q(r0 + 32, q[0]);
+            if (r0 + 16 < padded) block(r0 + 16, q[1]);
         }
         // over the four row groups; lane l then takes key block l / 16
         float total = 0.f;

@@ -471,6 +471,7 @@ int kv_accumulate_weights(const uint16_t *q, const float *lse, const uint16_t *k
     p.weight_out = weight_out; p.position = position;
     p.B = B; p.N = N; p.Hq = Hq; p.Hkv = Hkv;
     p.p_shift = __builtin_ctz((unsigned)P); p.max_pages = max_pages; p.num_pages = num_pages;
+    p.g_inv = Hq == Hkv ? 0u : (unsigned)((1ull << 32) / (unsigned)(Hq / Hkv) + 1);
     const long cap = (long)max_pages * P, hint = (long)max_kv_len + N;
     p.max_keys = (int)(hint < cap ? hint : cap);
     p.scale = scale > 0.f ? scale : 1.0f / sqrtf((float)D);

@@ -101,6 +101,7 @@ struct WeightParams {
     int32_t *position;
     int B, N, Hq, Hkv, p_shift, max_pages, num_pages;
     int max_keys;                // host-side bound of kv_len + path rows (sizes the launch only)
+    unsigned int g_inv;          // floor(2^32 / G) + 1: r / G is its high product with r < 2^11 (0: G = 1)
     float scale;
 };
 

@@ -421,6 +421,7 @@ def test_a_captured_step_replays():
     ws = torch.empty(T.shared_attention_workspace_size(3, 8, 8, 2, 128, 1), dtype=torch.uint8, device="cuda")
     we = torch.empty(T.evict_workspace_size(3, 2, w.page_table.shape[1], 16), dtype=torch.uint8, device="cuda")
     kc, vc = d["k_cache"].clone(), d["v_cache"].clone()
+    fixed = torch.full((3,), 192, dtype=torch.int32, device="cuda")   # shared pages: no row of them may move
 
     def step():
         kc.copy_(d["k_cache"])
@@ -433,7 +434,7 @@ def test_a_captured_step_replays():
                                 d["kv_len"], max_kv_len=w.max_kv_len, weight_out=w1)
         end = d["kv_len"] + alen
         T.kv_evict(w1, position, kc, vc, d["page_table"], end, end, max_kv_len=w.max_kv_len + 8, budget=230,
-                   recent=16, weight_out=w2, position_out=p2, kept_len=kept, workspace=we)
+                   recent=16, fixed_len=fixed, weight_out=w2, position_out=p2, kept_len=kept, workspace=we)
 
     def seen():
         torch.cuda.synchronize()
