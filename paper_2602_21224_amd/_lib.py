@@ -295,26 +295,35 @@ def kv_compact_accepted(k_tree, v_tree, k_cache, v_cache, page_table, kv_len, ac
 
 
 def _want_on(dev, t, name, dtypes, shape=None):
-    """_want, and on the device of the call's first tensor."""
+    """_want, and on the device (an index) of the call's first tensor."""
+    if (type(t) is torch.Tensor and t.dtype in dtypes and t.get_device() == dev
+            and t.is_contiguous() and (shape is None or t.shape == shape)):
+        return
     _want(t, name, dtypes, shape)
-    if t.device != dev:
-        raise ValueError(f"{name} is on {t.device}, expected {dev}")
+    if t.get_device() != dev:
+        raise ValueError(f"{name} is on {t.device}, expected cuda:{dev}")
+
+
+_current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
 
 
 def _call(what, dev, stream, own, *args):
-    """Call the C entry point on `dev` (made current for the call where it is not) and
-    on `stream`. `own`: tensors that the wrapper allocated, which the caching allocator
+    """Call the C entry point on device `dev` (made current for the call where it is not)
+    and on `stream`. `own`: tensors that the wrapper allocated, which the caching allocator
     must not hand out again before another stream than the current one is done with them."""
-    fn = getattr(load(), what)
-    if dev.index != torch.cuda.current_device():
+    fn = getattr(_lib or load(), what)
+    if dev != _current_device():
         with torch.cuda.device(dev):
             st = fn(*args, _stream(stream))
+    elif stream is None and _raw_stream is not None:
+        st = fn(*args, _raw_stream(dev))
     else:
         st = fn(*args, _stream(stream))
     if stream is not None:
         for t in own:
             t.record_stream(stream)
-    _check(st, what)
+    if st != 0:
+        _check(st, what)
 
 
 def shared_attention_workspace_size(B, N, Hq, Hkv, D, groups) -> int:
@@ -334,7 +343,7 @@ def tree_verify_attention_shared(q, k_tree, v_tree, k_cache, v_cache, page_table
     Hkv = k_tree.shape[2]
     num_pages, P = k_cache.shape[0], k_cache.shape[1]
     max_pages = page_table.shape[1]
-    dev = q.device
+    dev = q.get_device()
     _want(q, "q", _BF16)
     _want_on(dev, k_tree, "k_tree", _BF16, (B, N, Hkv, D))
     _want_on(dev, v_tree, "v_tree", _BF16, (B, N, Hkv, D))
@@ -353,17 +362,17 @@ def tree_verify_attention_shared(q, k_tree, v_tree, k_cache, v_cache, page_table
         _want_on(dev, shared_len, "shared_len", _I32, (groups,))
     own = []
     if out is None:
-        out = torch.empty((B, N, Hq, D), dtype=torch.bfloat16, device=dev)
+        out = torch.empty((B, N, Hq, D), dtype=torch.bfloat16, device=q.device)
         own.append(out)
     _want_on(dev, out, "out", _BF16, (B, N, Hq, D))
     if lse is None and want_lse:
-        lse = torch.empty((B, N, Hq), dtype=torch.float32, device=dev)
+        lse = torch.empty((B, N, Hq), dtype=torch.float32, device=q.device)
         own.append(lse)
     if lse is not None:
         _want_on(dev, lse, "lse", _F32, (B, N, Hq))
     if workspace is None:
         need = shared_attention_workspace_size(B, N, Hq, Hkv, D, groups)
-        workspace = torch.empty(max(need, 16), dtype=torch.uint8, device=dev)
+        workspace = torch.empty(max(need, 16), dtype=torch.uint8, device=q.device)
         own.append(workspace)
     _want_on(dev, workspace, "workspace", _U8)
     _call("tree_verify_attention_shared", dev, stream, own,
@@ -385,7 +394,7 @@ def kv_accumulate_weights(q, lse, k_cache, page_table, kv_len, accept_idx, accep
     B, N, Hq, D = q.shape
     num_pages, P, Hkv = k_cache.shape[0], k_cache.shape[1], k_cache.shape[2]
     max_pages = page_table.shape[1]
-    dev = q.device
+    dev = q.get_device()
     slots = (B, Hkv, max_pages * P)
     _want(q, "q", _BF16)
     _want_on(dev, lse, "lse", _F32, (B, N, Hq))
@@ -423,7 +432,7 @@ def kv_evict(weight, position, k_cache, v_cache, page_table, kv_len, seen, *, ma
     Returns (weight_out, position_out, kept_len)."""
     num_pages, P, Hkv, D = k_cache.shape
     B, max_pages = page_table.shape
-    dev = k_cache.device
+    dev = k_cache.get_device()
     slots = (B, Hkv, max_pages * P)
     _want(k_cache, "k_cache", _BF16)
     _want_on(dev, v_cache, "v_cache", _BF16, (num_pages, P, Hkv, D))
@@ -442,14 +451,14 @@ def kv_evict(weight, position, k_cache, v_cache, page_table, kv_len, seen, *, ma
     _want_on(dev, position_out, "position_out", _I32, slots)
     own = []
     if kept_len is None:
-        kept_len = torch.empty((B,), dtype=torch.int32, device=dev)
+        kept_len = torch.empty((B,), dtype=torch.int32, device=k_cache.device)
         own.append(kept_len)
     _want_on(dev, kept_len, "kept_len", _I32, (B,))
     if kept_len.data_ptr() == kv_len.data_ptr() and B > 0:
         raise ValueError("kept_len must not be kv_len itself")
     if workspace is None:
         need = evict_workspace_size(B, Hkv, max_pages, P)
-        workspace = torch.empty(max(need, 16), dtype=torch.uint8, device=dev)
+        workspace = torch.empty(max(need, 16), dtype=torch.uint8, device=k_cache.device)
         own.append(workspace)
     _want_on(dev, workspace, "workspace", _U8)
     _call("kv_evict", dev, stream, own,

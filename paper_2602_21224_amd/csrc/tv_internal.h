@@ -118,6 +118,8 @@ struct EvictParams {
     int B, Hkv, D, p_shift, max_pages, num_pages, budget, recent;
     int max_keys;                // host-side bound of kv_len (sizes the launch only)
     int vector_slots;            // four neighbouring slots can be loaded at once
+    int vector_out;              // and stored
+    int chunk_shift;             // log2 of a row's 16-byte pieces, or -1
     int move_here;               // the selecting workgroup moves the rows itself
 };
 
