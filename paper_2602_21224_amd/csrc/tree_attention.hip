@@ -60,7 +60,10 @@
 //   * How many keys are taken together is the kernel's choice: whole tiles, at
 //     most what the shortest sequence of the group has, so shared tiles need no
 //     mask and the sequences' own tiles start at a tile. Results do not depend
-//     on it beyond rounding.
+//     on it beyond rounding. A group whose rows fill no fewer blocks together
+//     than its sequences' blocks, each by itself, takes none: every block visits
+//     every tile once either way, and rows of one piece need no joining (16
+//     sequences x 512 rows over 16384 shared tokens 665 us shared, 611 not).
 //   * Every row of such a group has two results to be joined, one per kind. A
 //     unit that one workgroup covers leaves a whole normalised row (shared: in
 //     the workspace, own: in out) and its log-sum-exp, a split unit leaves pieces
@@ -80,6 +83,8 @@ constexpr int NS = 4;                  // ring stages (a power of two: stage = t
 constexpr int kPageCache = 512;        // page ids cached in LDS per segment window
 constexpr float kNegInf = -__builtin_huge_valf();
 constexpr float kLn2 = 0.693147180559945309f;
+constexpr int kSharedWaves = 8;         // of a workgroup of the shared-prefix kernels
+constexpr int kSharedTileCost = 3;      // of a tile of a shared unit, in tiles of own units of up to 64 rows
 constexpr float kRescaleSlack = 8.f;   // keep a stale running max while new scores stay within 2^8 of it
 
 typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
@@ -151,7 +156,8 @@ __shared__ int g_vcum[kMaxGroups + kMaxBatchShared + 1];
 __shared__ int g_slen[kMaxBatchShared];          // clamped prefix length per sequence
 __shared__ int g_ncum[kMaxBatchShared + 1];      // real nodes of the sequences before b
 __shared__ int g_gtiles[kMaxGroups];             // tiles taken together (first: shortest prefix of the group)
-__shared__ int g_first[kMaxGroups], g_last[kMaxGroups];   // first and last sequence that has nodes
+__shared__ int g_first[kMaxGroups];              // first sequence that has nodes
+__shared__ int g_blocks[kMaxGroups];             // row blocks of the sequences, each by itself
 __shared__ unsigned short g_gstart[kMaxGroups + 1];
 __shared__ unsigned short g_group[kMaxBatchShared];       // group of a sequence, or kMaxGroups
 
@@ -282,9 +288,24 @@ __device__ __forceinline__ int shared_tiles_of(int b) {
     return s < kMaxGroups ? g_gtiles[s] : 0;
 }
 
+template <int D>
+struct OwnGeo {
+    static constexpr int kKeys = 4096 / D;             // per tile
+    static constexpr int kLoads = 8;                   // 1 KB loads of K (and of V) per tile
+    static constexpr int kKeysPerLoad = 512 / D;
+    static constexpr int kHalfBytes = 8192;            // of K, and of V
+};
+
+// Real tiles of a sequence's units: prefix positions from `from` on, then the nodes.
+template <int D>
+__device__ __forceinline__ int own_tiles(int L, int from, int nodes) {
+    return nodes == 0 ? 0 : (L - from + nodes + OwnGeo<D>::kKeys - 1) / OwnGeo<D>::kKeys;
+}
+
 // The tables of a batch with shared prefixes, by all threads; w = 0 leaves what
-// the joining kernel needs of them in the workspace.
-template <int NT>
+// the joining kernel needs of them in the workspace. D_OWN > 0: the sequences' own
+// keys are units of tree_attention_own.h for that head size.
+template <int NT, int D_OWN>
 __device__ void build_shared_tables(const AttnParams &p, int w) {
     const int tid = threadIdx.x, lane = tid & (kWave - 1);
     if (tid < kWave) {
@@ -313,7 +334,7 @@ __device__ void build_shared_tables(const AttnParams &p, int w) {
     for (int s = tid; s < p.groups; s += NT) {
         g_gtiles[s] = 0x7FFFFFFF;
         g_first[s] = 0x7FFFFFFF;
-        g_last[s] = -1;
+        g_blocks[s] = 0;
     }
     __syncthreads();
     for (int b = tid; b < p.B; b += NT) {
@@ -330,12 +351,13 @@ __device__ void build_shared_tables(const AttnParams &p, int w) {
         if (s < kMaxGroups && g_ncum[b + 1] > g_ncum[b]) {
             atomicMin(&g_gtiles[s], g_slen[b]);
             atomicMin(&g_first[s], b);
-            atomicMax(&g_last[s], b);
+            atomicAdd(&g_blocks[s], D_OWN ? 1 : row_blocks_of((g_ncum[b + 1] - g_ncum[b]) * p.G, p));
         }
     }
     __syncthreads();
     for (int s = tid; s < p.groups; s += NT)
-        g_gtiles[s] = g_last[s] > g_first[s] ? max(min(g_gtiles[s], p.shared_len[s]), 0) / KT : 0;
+        g_gtiles[s] = g_blocks[s] > (D_OWN ? 1 : row_blocks_of(group_rows(s, p), p))
+                          ? max(min(g_gtiles[s], p.shared_len[s]), 0) / KT : 0;
     __syncthreads();
     if (tid < kWave) {
         int carry = 0;
@@ -347,9 +369,13 @@ __device__ void build_shared_tables(const AttnParams &p, int w) {
                 if (g_gtiles[v] > 0)
                     t = p.Hkv * row_blocks_of(group_rows(v, p), p) * (p.setup_tiles + g_gtiles[v]);
             } else if (v < nv) {
-                const int b = v - p.groups;
-                t = p.Hkv * tiles_per_head((g_slen[b] + KT - 1) / KT - shared_tiles_of(b),
-                                           (g_ncum[b + 1] - g_ncum[b]) * p.G, p);
+                const int b = v - p.groups, n = g_ncum[b + 1] - g_ncum[b];
+                if constexpr (D_OWN > 0) {
+                    const int own = own_tiles<D_OWN>(g_slen[b], shared_tiles_of(b) * KT, n);
+                    t = own > 0 ? p.Hkv * (own + 1) : 0;
+                } else {
+                    t = p.Hkv * tiles_per_head((g_slen[b] + KT - 1) / KT - shared_tiles_of(b), n * p.G, p);
+                }
             }
             const int x = wave_scan_sum(t, lane);
             if (v < nv) g_vcum[v] = carry + x - t;
@@ -1013,19 +1039,34 @@ __device__ __forceinline__ size_t group_node(int s, int ord, const AttnParams &p
 // A group of R rows behind X rows of groups before it has at most
 // floor((X + R) / block) - floor(X / block) + 1 row blocks, so with one more per
 // group before it the blocks of all groups get numbers of their own.
+__device__ __forceinline__ int own_blocks(const AttnParams &p) {
+    return (p.N * p.G + p.own_rows - 1) / p.own_rows;
+}
 __device__ __forceinline__ int own_unit(int b, int g, int rb, const AttnParams &p) {
-    return (b * p.Hkv + g) * row_blocks_of(p.N * p.G, p) + rb;
+    return (b * p.Hkv + g) * own_blocks(p) + rb;
 }
 __device__ __forceinline__ int shared_unit_of(int block, int g, const AttnParams &p) {
-    return p.B * p.Hkv * row_blocks_of(p.N * p.G, p) + block * p.Hkv + g;
+    return p.B * p.Hkv * own_blocks(p) + block * p.Hkv + g;
 }
 __device__ __forceinline__ int shared_unit(int s, int g, int rb, const AttnParams &p) {
     return shared_unit_of(g_ncum[g_gstart[s]] * p.G / p.rows_per_block + s + rb, g, p);
 }
 
-template <int D, int NW, bool SMALL, bool NARROW, bool WHOLE, bool SHARED = false>
+}  // namespace
+}  // namespace tv
+
+#include "tree_attention_own.h"
+
+namespace tv {
+namespace {
+
+// SHARED: a batch with shared prefixes; RT > 0: its sequences' own keys are units of
+// at most RT x 16 rows that some of the workgroups take wave by wave, the others
+// share the groups' units.
+template <int D, int NW, bool SMALL, bool NARROW, bool WHOLE, bool SHARED = false, int RT = 0>
 __global__ __launch_bounds__(NW * kWave) void tree_attention_kernel(AttnParams p) {
     static_assert(!SHARED || (!NARROW && !WHOLE), "shared prefixes: wide units, split");
+    static_assert(RT == 0 || (SHARED && NW == kSharedWaves), "own units: of batches with shared prefixes");
     using Gm = Geo<D>;
     using Issue = TileIssue<D, NW, SMALL>;
     constexpr int NT = NW * kWave;
@@ -1038,17 +1079,38 @@ __global__ __launch_bounds__(NW * kWave) void tree_attention_kernel(AttnParams p
     const int wave_u = __builtin_amdgcn_readfirstlane(tid / kWave);
     const int half = lane >> 5;
     const int col = lane & 31;
-    const int w = xcd_contiguous_id(blockIdx.x, p.num_wg);
+    int w = xcd_contiguous_id(blockIdx.x, p.num_wg);
 
-    if constexpr (SHARED) build_shared_tables<NT>(p, w);
+    if constexpr (SHARED) build_shared_tables<NT, RT ? D : 0>(p, w);
     else build_cumulative<NT>(p);
 
-    const int total = SHARED ? g_vcum[p.groups + p.B] : g_cum[p.B];
+    int num_wg = p.num_wg;
+    int total = SHARED ? g_vcum[p.groups + p.B] : g_cum[p.B];
+    if constexpr (RT > 0) {
+        // Workgroups are divided by the work of the two kinds, in multiples of the XCDs
+        const int shared = g_vcum[p.groups], own = total - shared;
+        const int eighths = num_wg / kNumXcd;
+        int ns = 0;
+        if (shared > 0) {
+            const long long a = (long long)shared * kSharedTileCost, both = a + own;
+            ns = min(max((int)((a * eighths + both / 2) / both), 1), eighths - 1) * kNumXcd;
+        }
+        if ((int)blockIdx.x >= ns) {
+            const int o = xcd_contiguous_id(blockIdx.x - ns, num_wg - ns);
+            own_shares<D, RT>(p, o * NW + wave_u, (num_wg - ns) * NW);
+            w = ns + o;
+            total = 0;
+        } else {
+            w = xcd_contiguous_id(blockIdx.x, ns);
+            total = shared;
+        }
+        num_wg = ns;
+    }
     // Workgroup u < nw takes virtual tiles [share_start(u), share_start(u + 1)):
     // shares differ by at most one tile and none is empty (nw <= total), so the
     // pieces of a split unit sit in consecutive workgroups. Workgroups past nw
     // (only when the length hint overstated the work) have nothing to do.
-    const int nw = min(p.num_wg, total);
+    const int nw = min(num_wg, total);
     auto share_start = [&](int u) { return (int)(((long long)min(u, nw) * total) / max(nw, 1)); };
     auto share_of = [&](int t) { return (int)(((long long)(t + 1) * nw - 1) / total); };
     int start = share_start(w), end = share_start(w + 1);
@@ -1090,7 +1152,7 @@ __global__ __launch_bounds__(NW * kWave) void tree_attention_kernel(AttnParams p
                 if (g_vcum[mid] <= pos) lo = mid; else hi = mid - 1;
             }
             off = pos - g_vcum[lo];
-            if (lo < p.groups) {
+            if (RT > 0 || lo < p.groups) {
                 sg = lo;
                 b = g_first[sg];
                 ntp = g_gtiles[sg];
@@ -1555,6 +1617,7 @@ __global__ __launch_bounds__(NW * kWave) void tree_attention_kernel(AttnParams p
         __syncthreads();                   // the ring is refilled by the next piece
     }
 
+
     // Rows of padding nodes (at or past a sequence's node count) are not part
     // of any unit: write them as zeros with lse -inf, a few nodes per workgroup.
     if (p.num_nodes) {
@@ -1642,7 +1705,7 @@ __global__ __launch_bounds__(256) void shared_join_kernel(AttnParams p) {
     const int g = h / p.G;
     const int own_row = i * p.G + h % p.G;
     const int group_row = sq[0] * p.G + own_row;
-    const int *own = p.ws_unit + 2 * own_unit(b, g, own_row / p.rows_per_block, p);
+    const int *own = p.ws_unit + 2 * own_unit(b, g, own_row / p.own_rows, p);
     const int *shr = p.ws_unit + 2 * shared_unit_of(sq[1] + group_row / p.rows_per_block, g, p);
     const bool shared = sq[2] > 0;
     const int own_first = own[0], own_last = own[1];
@@ -1660,7 +1723,8 @@ __global__ __launch_bounds__(256) void shared_join_kernel(AttnParams p) {
         for (int e = 0; e < 8; ++e) acc[e] = acc[e] * sc + wt * (float)v[e];
         M = Mn;
     };
-    auto add_unit = [&](int first, int last, int rl, const uint16_t *whole, const float *lse2) {
+    auto add_unit = [&](int first, int last, int rl, int slot_rows, const uint16_t *ws_o, const float *ws_ml,
+                        const uint16_t *whole, const float *lse2) {
         if (first < 0) {
             add(whole + row * D, lse2[row], 1.f);
             return;
@@ -1668,13 +1732,14 @@ __global__ __launch_bounds__(256) void shared_join_kernel(AttnParams p) {
         #pragma unroll 4
         for (int u = first >> 1; u <= last; ++u) {
             // the first piece may sit in slot 1 of its workgroup; later ones start a share
-            const size_t r = (size_t)(u == (first >> 1) ? first : u * 2) * p.rows_per_block + rl;
-            const f32x2 ml = *reinterpret_cast<const f32x2 *>(p.ws_ml + r * 2);
-            add(p.ws_o + r * D, ml[0], ml[1]);
+            const size_t r = (size_t)(u == (first >> 1) ? first : u * 2) * slot_rows + rl;
+            const f32x2 ml = *reinterpret_cast<const f32x2 *>(ws_ml + r * 2);
+            add(ws_o + r * D, ml[0], ml[1]);
         }
     };
-    if (shared) add_unit(shr[0], shr[1], group_row % p.rows_per_block, p.ws_so, p.ws_lse2);
-    add_unit(own_first, own_last, own_row % p.rows_per_block, p.out, p.ws_lse2 + rows);
+    if (shared)
+        add_unit(shr[0], shr[1], group_row % p.rows_per_block, p.rows_per_block, p.ws_o, p.ws_ml, p.ws_so, p.ws_lse2);
+    add_unit(own_first, own_last, own_row % p.own_rows, p.own_rows, p.own_o, p.own_ml, p.out, p.ws_lse2 + rows);
     const float inv = den > 0.f ? 1.f / den : 0.f;
     bf16x8 o;
     #pragma unroll
@@ -1727,10 +1792,20 @@ hipError_t launch_d(const AttnParams &p, int waves, hipStream_t s) {
 
 template <int D>
 hipError_t launch_shared_d(const AttnParams &p, hipStream_t s) {
-    constexpr int NW = 8;
-    const auto kernel = p.small_pages ? tree_attention_kernel<D, NW, true, false, false, true>
-                                      : tree_attention_kernel<D, NW, false, false, false, true>;
-    const hipError_t e = launch_kernel(kernel, dim3(p.num_wg), dim3(NW * kWave), s, p);
+    auto go = [&](auto rt) {
+        constexpr int RT = decltype(rt)::value;
+        const auto kernel = p.small_pages ? tree_attention_kernel<D, kSharedWaves, true, false, false, true, RT>
+                                          : tree_attention_kernel<D, kSharedWaves, false, false, false, true, RT>;
+        return launch_kernel(kernel, dim3(p.num_wg), dim3(kSharedWaves * kWave), s, p);
+    };
+    hipError_t e;
+    switch (p.own_tiles16) {
+        case 1: e = go(std::integral_constant<int, 1>{}); break;
+        case 2: e = go(std::integral_constant<int, 2>{}); break;
+        case 3: e = go(std::integral_constant<int, 3>{}); break;
+        case 4: e = go(std::integral_constant<int, 4>{}); break;
+        default: e = go(std::integral_constant<int, 0>{}); break;
+    }
     if (e != hipSuccess) return e;
     const size_t rows = (size_t)p.B * p.N * p.Hq, per = 256 / (D / 8);
     return launch_kernel(shared_join_kernel<D>, dim3((unsigned)((rows + per - 1) / per)), dim3(256), s, p);

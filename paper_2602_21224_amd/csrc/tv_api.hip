@@ -112,38 +112,50 @@ AttnWorkspace attn_workspace(const AttnShape &s, int D, int max_wg) {
 }
 
 // Batches with shared prefixes run workgroups of eight waves throughout: a
-// group's rows are many, and a period of few rows is bound by its tile loads,
-// which eight waves issue as fast as four.
-AttnShape shared_shape(int N, int Hq, int Hkv) {
-    AttnShape s = attn_shape(N, Hq, Hkv);
-    s.waves = 8;
-    s.rows_per_block = s.waves * tv::kRowsPerWave;
-    s.row_blocks = (s.rows + s.rows_per_block - 1) / s.rows_per_block;
-    s.tree_tiles_all = s.row_blocks * ((N + tv::kKeyTile - 1) / tv::kKeyTile);   // at most
+// group's rows are many. Own units of at most 64 rows are taken wave by wave
+// (tree_attention_own.h), larger ones in row blocks like the shared ones.
+struct SharedShape {
+    AttnShape wide;
+    int own_rows, own_tiles16, own_blocks;
+};
+
+SharedShape shared_shape(int N, int Hq, int Hkv) {
+    SharedShape s;
+    s.wide = attn_shape(N, Hq, Hkv);
+    s.wide.waves = 8;
+    s.wide.rows_per_block = s.wide.waves * tv::kRowsPerWave;
+    s.wide.row_blocks = (s.wide.rows + s.wide.rows_per_block - 1) / s.wide.rows_per_block;
+    s.wide.tree_tiles_all = s.wide.row_blocks * ((N + tv::kKeyTile - 1) / tv::kKeyTile);   // at most
+    s.own_tiles16 = s.wide.rows <= 64 ? (s.wide.rows + 15) / 16 : 0;
+    s.own_rows = s.own_tiles16 ? 16 * s.own_tiles16 : s.wide.rows_per_block;
+    s.own_blocks = s.own_tiles16 ? 1 : s.wide.row_blocks;
     return s;
 }
 
 // Most row blocks per KV head that the groups' shared units can have together.
-long shared_blocks(const AttnShape &s, int B, int groups) {
-    return ((long)B * s.rows + s.rows_per_block - 1) / s.rows_per_block + groups;
+long shared_blocks(const SharedShape &s, int B, int groups) {
+    return ((long)B * s.wide.rows + s.wide.rows_per_block - 1) / s.wide.rows_per_block + groups;
 }
 
 struct SharedWorkspace {
     AttnWorkspace split;
-    size_t so, lse2, unit, seq, total;       // byte offsets, and the whole
+    size_t so, lse2, unit, seq, own_o, own_ml, total;       // byte offsets, and the whole
 };
 
-SharedWorkspace shared_workspace(const AttnShape &s, int B, int N, int Hq, int Hkv, int D, int groups,
+SharedWorkspace shared_workspace(const SharedShape &s, int B, int N, int Hq, int Hkv, int D, int groups,
                                  int max_wg) {
     SharedWorkspace w;
     const size_t rows = (size_t)B * N * Hq;
-    const size_t units = ((size_t)B * s.row_blocks + (size_t)shared_blocks(s, B, groups)) * Hkv;
-    w.split = attn_workspace(s, D, max_wg);
+    const size_t units = ((size_t)B * s.own_blocks + (size_t)shared_blocks(s, B, groups)) * Hkv;
+    const size_t own = s.own_tiles16 ? (size_t)max_wg * s.wide.waves * 2 * s.own_rows : 0;   // rows of a wave's slots
+    w.split = attn_workspace(s.wide, D, max_wg);
     w.so = w.split.o_bytes + w.split.ml_bytes;
     w.lse2 = w.so + round_up(rows * D * sizeof(uint16_t), 256);
     w.unit = w.lse2 + round_up(rows * 2 * sizeof(float), 256);
     w.seq = w.unit + round_up(units * 2 * sizeof(int32_t), 256);
-    w.total = w.seq + round_up((size_t)B * 4 * sizeof(int32_t), 256) + 256;
+    w.own_o = w.seq + round_up((size_t)B * 4 * sizeof(int32_t), 256);
+    w.own_ml = w.own_o + round_up(own * D * sizeof(uint16_t), 256);
+    w.total = w.own_ml + round_up(own * 2 * sizeof(float), 256) + 256;
     return w;
 }
 
@@ -406,22 +418,26 @@ int tree_verify_attention_shared(
     if (!aligned16(q) || !aligned16(k_tree) || !aligned16(v_tree) || !aligned16(k_cache) ||
         !aligned16(v_cache) || !aligned16(out) || !aligned16(workspace))
         return TV_ERR_ALIGN;
-    const AttnShape s = shared_shape(N, Hq, Hkv);
+    const SharedShape s = shared_shape(N, Hq, Hkv);
     const int max_wg = cu_count() * kWgPerCu;
     const SharedWorkspace ws = shared_workspace(s, B, N, Hq, Hkv, D, groups, max_wg);
     if (workspace_bytes < ws.total) return TV_ERR_WORKSPACE;
 
-    // the (virtual) tile count of the whole launch must fit in int32 for any kv_len
+    // the (virtual) tile count of the whole launch must fit in int32 for any kv_len (own
+    // tiles of units of few rows: half as many keys, at least)
     const long max_len = (long)max_pages * P;
-    const long blocks = (long)B * s.row_blocks + shared_blocks(s, B, groups);
+    const long blocks = 2l * B * s.wide.row_blocks + shared_blocks(s, B, groups);
     auto tiles = [&](long len) {
-        return Hkv * (blocks * ((len + tv::kKeyTile - 1) / tv::kKeyTile + kSetupTiles) + (long)B * s.tree_tiles_all);
+        return Hkv * (blocks * ((len + tv::kKeyTile - 1) / tv::kKeyTile + kSetupTiles) +
+                      2l * B * s.wide.tree_tiles_all);
     };
     if (tiles(max_len) >= (1l << 30)) return TV_ERR_SHAPE;
     if (!device_ok()) return TV_ERR_DEVICE;
     long num_wg = tiles(max_kv_len < max_len ? max_kv_len : max_len) / kMinShareTiles;
     if (num_wg < 1) num_wg = 1;
     if (num_wg > max_wg) num_wg = max_wg;
+    // the two kinds of units divide the workgroups in multiples of the XCDs, both at least one
+    if (s.own_tiles16) num_wg = num_wg < 2 * tv::kNumXcd ? 2 * tv::kNumXcd : num_wg / tv::kNumXcd * tv::kNumXcd;
 
     tv::AttnParams p{};
     p.q = q; p.k_tree = k_tree; p.v_tree = v_tree; p.k_cache = k_cache; p.v_cache = v_cache;
@@ -439,8 +455,11 @@ int tree_verify_attention_shared(
     p.ws_lse2 = reinterpret_cast<float *>(base + ws.lse2);
     p.ws_unit = reinterpret_cast<int32_t *>(base + ws.unit);
     p.ws_seq = reinterpret_cast<int32_t *>(base + ws.seq);
+    p.own_rows = s.own_rows; p.own_tiles16 = s.own_tiles16;
+    p.own_o = s.own_tiles16 ? reinterpret_cast<uint16_t *>(base + ws.own_o) : p.ws_o;
+    p.own_ml = s.own_tiles16 ? reinterpret_cast<float *>(base + ws.own_ml) : p.ws_ml;
     p.group_start = group_start; p.shared_len = shared_len; p.groups = groups;
-    p.rows_per_block = s.rows_per_block;
+    p.rows_per_block = s.wide.rows_per_block;
     p.setup_tiles = kSetupTiles;
     p.small_pages = P < 1024 / (2 * D) ? 1 : 0;
     p.num_wg = (int)num_wg;

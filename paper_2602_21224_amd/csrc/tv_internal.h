@@ -89,6 +89,11 @@ struct AttnParams {
     float *ws_lse2;              // [2][B * N * Hq] log-sum-exp (base 2) of whole units: shared, own
     int32_t *ws_unit;            // [units][2]: slot of the first piece (-1: whole), workgroup of the last
     int32_t *ws_seq;             // [B][4] per sequence: see build_shared_tables
+    // the sequences' own units: rows of one, which may be those of ws_o's slots, or 16
+    // per row tile that a wave takes by itself (own_tiles16 > 0)
+    int own_rows, own_tiles16;
+    uint16_t *own_o;             // [slots][own_rows][D] bf16 pieces (normalised)
+    float *own_ml;               // [slots][own_rows][2] (max, sum)
 };
 
 // Launch parameters of the accumulated attention weights (all sizes in elements).

@@ -17,7 +17,7 @@ pytestmark = pytest.mark.gpu
 
 def attend(T, w, start, shared, d=None, **kw):
     d = d or U.upload(w)
-    i32 = lambda a: None if a is None else U.dev(np.asarray(a, np.int32))  # noqa: E731
+    i32 = lambda a: a if a is None or isinstance(a, torch.Tensor) else U.dev(np.asarray(a, np.int32))  # noqa: E731
     return T.tree_verify_attention_shared(
         d["q"], d["k_tree"], d["v_tree"], d["k_cache"], d["v_cache"], d["page_table"], d["kv_len"], d["parent"],
         i32(start), i32(shared), max_kv_len=w.max_kv_len, num_nodes=d["num_nodes"], **kw)
@@ -393,9 +393,11 @@ def test_calls_on_other_streams():
     ref = copy()
     kept = evict(T, s, ref, 256, 30)
     two = [copy(), copy()]
+    # inputs live until the other streams are done with them
+    start, shared = U.dev(np.array([0, 4], np.int32)), U.dev(np.array([512], np.int32))
     torch.cuda.synchronize()
     streams = [torch.cuda.Stream(), torch.cuda.Stream()]
-    outs = [attend(T, w, [0, 4], [512], d, stream=st) for st in streams]
+    outs = [attend(T, w, start, shared, d, stream=st) for st in streams]
     kepts = [evict(T, s, x, 256, 30, stream=st) for x, st in zip(two, streams)]
     torch.cuda.synchronize()
     for (o, z), x, k in zip(outs, two, kepts):
