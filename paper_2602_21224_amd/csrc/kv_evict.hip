@@ -37,22 +37,8 @@ constexpr int kFewPieces = 8;       // 16-byte pieces (of K and of V) per thread
 template <int NT, int ITER>
 constexpr int kSlots = NT * 4 * ITER;
 
-template <int CTRL, int ROWS>
-__device__ __forceinline__ int dpp_add(int x) {
-    return x + __builtin_amdgcn_update_dpp(0, x, CTRL, ROWS, 0xF, false);
-}
-// Inclusive sum over the lanes: within rows of 16 by shifts of 1, 2, 4 and 8, then each
-// row's last lane onto the next row, and lane 31 onto the upper half.
-__device__ __forceinline__ int wave_prefix(int x) {
-    x = dpp_add<0x111, 0xF>(x);
-    x = dpp_add<0x112, 0xF>(x);
-    x = dpp_add<0x114, 0xF>(x);
-    x = dpp_add<0x118, 0xF>(x);
-    x = dpp_add<0x142, 0xA>(x);
-    return dpp_add<0x143, 0xC>(x);
-}
 __device__ __forceinline__ int wave_sum(int x) {
-    return __builtin_amdgcn_readlane(wave_prefix(x), kWave - 1);
+    return __builtin_amdgcn_readlane(wave_prefix_sum(x), kWave - 1);
 }
 // Set bits, of four per lane, in the lanes before this one, and in all of them.
 __device__ __forceinline__ int bits_before(unsigned int nibble, int &all) {
@@ -289,7 +275,7 @@ __global__ __launch_bounds__(NT) void evict_select_kernel(EvictParams p) {
             c[i] = i < per ? hist[d][bins - 1 - (tid * per + i)] : 0;
             sum += c[i];
         }
-        const int incl = wave_prefix(sum);
+        const int incl = wave_prefix_sum(sum);
         int all;
         int before = exchange(1 + d, __builtin_amdgcn_readlane(incl, kWave - 1), all) + incl - sum;
         #pragma unroll

@@ -84,7 +84,6 @@ constexpr int kPageCache = 512;        // page ids cached in LDS per segment win
 constexpr float kNegInf = -__builtin_huge_valf();
 constexpr float kLn2 = 0.693147180559945309f;
 constexpr int kSharedWaves = 8;         // of a workgroup of the shared-prefix kernels
-constexpr int kSharedTileCost = 3;      // of a tile of a shared unit, in tiles of own units of up to 64 rows
 constexpr float kRescaleSlack = 8.f;   // keep a stale running max while new scores stay within 2^8 of it
 
 typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
@@ -259,24 +258,6 @@ __device__ void build_cumulative(const AttnParams &p) {
     __syncthreads();
 }
 
-// Inclusive prefix maximum or sum over a wave.
-__device__ __forceinline__ int wave_scan_max(int x, int lane) {
-    #pragma unroll
-    for (int off = 1; off < kWave; off <<= 1) {
-        const int y = __shfl_up(x, off);
-        if (lane >= off) x = max(x, y);
-    }
-    return x;
-}
-__device__ __forceinline__ int wave_scan_sum(int x, int lane) {
-    #pragma unroll
-    for (int off = 1; off < kWave; off <<= 1) {
-        const int y = __shfl_up(x, off);
-        if (lane >= off) x += y;
-    }
-    return x;
-}
-
 // Query rows per KV head of group s: those of its sequences' real nodes.
 __device__ __forceinline__ int group_rows(int s, const AttnParams &p) {
     return (g_ncum[g_gstart[s + 1]] - g_ncum[g_gstart[s]]) * p.G;
@@ -296,6 +277,21 @@ struct OwnGeo {
     static constexpr int kHalfBytes = 8192;            // of K, and of V
 };
 
+// Places (virtual tiles) of an own tile; a unit has one more in front, for its start.
+constexpr int kOwnTile = 2;
+
+// Time of a (virtual) tile of the shared units, which is bound by its products, in
+// places of own units, whose tiles are bound by their loads and, of several row tiles,
+// by their latency: what divides the workgroups between the two. us per call with 2, 3
+// and 4 own tiles per shared one: head size 128, 16 rows: 64 sequences of one row over
+// 4096 shared tokens 40.0, 35.3, 33.4, 16 of 8 rows over 16384 57.5, 55.6, 58.4, of 12
+// rows over 1024 56.9, 49.4, 49.7; 32 rows 39.0, 38.5, 41.3; 48 rows 44.2, 47.8, 49.1;
+// head size 64: 27.1, 24.9, 26.2 and 26.1, 24.7, 25.4.
+template <int D, int RT>
+constexpr int shared_tile_cost() {
+    return D == 64 ? 3 * kOwnTile : RT == 1 ? 7 * kOwnTile / 2 : 2 * kOwnTile;
+}
+
 // Real tiles of a sequence's units: prefix positions from `from` on, then the nodes.
 template <int D>
 __device__ __forceinline__ int own_tiles(int L, int from, int nodes) {
@@ -307,13 +303,15 @@ __device__ __forceinline__ int own_tiles(int L, int from, int nodes) {
 // keys are units of tree_attention_own.h for that head size.
 template <int NT, int D_OWN>
 __device__ void build_shared_tables(const AttnParams &p, int w) {
+    static_assert(NT >= kMaxGroups, "one thread per group");
     const int tid = threadIdx.x, lane = tid & (kWave - 1);
+    const int promised = tid < p.groups ? p.shared_len[tid] : 0;    // asked for early
     if (tid < kWave) {
         int top = 0;                     // a start counts as the largest before it
         for (int s0 = 0; s0 <= p.groups && p.groups > 0; s0 += kWave) {
             const int s = s0 + lane;
             const int x = s <= p.groups ? min(max(p.group_start[s], 0), p.B) : 0;
-            const int y = max(top, wave_scan_max(x, lane));
+            const int y = max(top, wave_prefix_max(x));
             if (s <= p.groups) g_gstart[s] = (unsigned short)y;
             top = __shfl(y, kWave - 1);
         }
@@ -322,7 +320,7 @@ __device__ void build_shared_tables(const AttnParams &p, int w) {
         for (int b0 = 0; b0 < p.B; b0 += kWave) {
             const int b = b0 + lane;
             const int n = b < p.B ? nodes_of(b, p) : 0;
-            const int x = wave_scan_sum(n, lane);
+            const int x = wave_prefix_sum(n);
             if (b < p.B) {
                 g_ncum[b] = carry + x - n;
                 g_slen[b] = clamp_len(p.kv_len[b], p);
@@ -331,10 +329,10 @@ __device__ void build_shared_tables(const AttnParams &p, int w) {
         }
         if (lane == 0) g_ncum[p.B] = carry;
     }
-    for (int s = tid; s < p.groups; s += NT) {
-        g_gtiles[s] = 0x7FFFFFFF;
-        g_first[s] = 0x7FFFFFFF;
-        g_blocks[s] = 0;
+    if (tid < p.groups) {
+        g_gtiles[tid] = 0x7FFFFFFF;
+        g_first[tid] = 0x7FFFFFFF;
+        g_blocks[tid] = 0;
     }
     __syncthreads();
     for (int b = tid; b < p.B; b += NT) {
@@ -355,9 +353,9 @@ __device__ void build_shared_tables(const AttnParams &p, int w) {
         }
     }
     __syncthreads();
-    for (int s = tid; s < p.groups; s += NT)
-        g_gtiles[s] = g_blocks[s] > (D_OWN ? 1 : row_blocks_of(group_rows(s, p), p))
-                          ? max(min(g_gtiles[s], p.shared_len[s]), 0) / KT : 0;
+    if (tid < p.groups)
+        g_gtiles[tid] = g_blocks[tid] > (D_OWN ? 1 : row_blocks_of(group_rows(tid, p), p))
+                            ? max(min(g_gtiles[tid], promised), 0) / KT : 0;
     __syncthreads();
     if (tid < kWave) {
         int carry = 0;
@@ -372,12 +370,12 @@ __device__ void build_shared_tables(const AttnParams &p, int w) {
                 const int b = v - p.groups, n = g_ncum[b + 1] - g_ncum[b];
                 if constexpr (D_OWN > 0) {
                     const int own = own_tiles<D_OWN>(g_slen[b], shared_tiles_of(b) * KT, n);
-                    t = own > 0 ? p.Hkv * (own + 1) : 0;
+                    t = own > 0 ? p.Hkv * (own * kOwnTile + 1) : 0;
                 } else {
                     t = p.Hkv * tiles_per_head((g_slen[b] + KT - 1) / KT - shared_tiles_of(b), n * p.G, p);
                 }
             }
-            const int x = wave_scan_sum(t, lane);
+            const int x = wave_prefix_sum(t);
             if (v < nv) g_vcum[v] = carry + x - t;
             carry += __shfl(x, kWave - 1);
         }
@@ -1092,7 +1090,7 @@ __global__ __launch_bounds__(NW * kWave) void tree_attention_kernel(AttnParams p
         const int eighths = num_wg / kNumXcd;
         int ns = 0;
         if (shared > 0) {
-            const long long a = (long long)shared * kSharedTileCost, both = a + own;
+            const long long a = (long long)shared * shared_tile_cost<D, RT>(), both = a + own;
             ns = min(max((int)((a * eighths + both / 2) / both), 1), eighths - 1) * kNumXcd;
         }
         if ((int)blockIdx.x >= ns) {
@@ -1244,6 +1242,9 @@ __global__ __launch_bounds__(NW * kWave) void tree_attention_kernel(AttnParams p
         // before the first score product.
         const int row = rb * p.rows_per_block + wave_u * kRowsPerWave + col;
         const bool row_ok = row < rows_b;
+        // a wave without rows loads its share of the tiles and computes nothing (the
+        // instances for whole batches choose fewer waves instead)
+        const bool idle = rb * p.rows_per_block + wave_u * kRowsPerWave >= rows_b;
         const int qrow = row_ok ? row : rb * p.rows_per_block;
         int node = qrow / p.G;
         const int hq = g * p.G + qrow % p.G;
@@ -1437,8 +1438,9 @@ __global__ __launch_bounds__(NW * kWave) void tree_attention_kernel(AttnParams p
             auto run = [&](auto prev, auto cur) {
                 constexpr bool P_ = decltype(prev)::value, C_ = decltype(cur)::value;
                 const int jj = j;
-                tile_period<D, P_, C_>(st, s0, s1, C_ ? kaddr_of(ta + jj) : 0u,
-                                       P_ ? vaddr_of(ta + jj - 1) : 0u, mk, p.scale_log2);
+                if (!SHARED || !idle)
+                    tile_period<D, P_, C_>(st, s0, s1, C_ ? kaddr_of(ta + jj) : 0u,
+                                           P_ ? vaddr_of(ta + jj - 1) : 0u, mk, p.scale_log2);
                 if (C_) close_period(jj);
             };
             // Before the last PV: V of the last tile has landed for every wave.
@@ -1700,21 +1702,28 @@ __global__ __launch_bounds__(256) void shared_join_kernel(AttnParams p) {
     const size_t rows = (size_t)p.B * p.N * p.Hq;
     if (row >= rows) return;
     const int h = (int)(row % p.Hq), i = (int)(row / p.Hq % p.N), b = (int)(row / ((size_t)p.Hq * p.N));
-    const i32x4 sq = reinterpret_cast<const i32x4 *>(p.ws_seq)[b];
-    if (i >= sq[3]) return;                         // padding: written by the main kernel
     const int g = h / p.G;
     const int own_row = i * p.G + h % p.G;
-    const int group_row = sq[0] * p.G + own_row;
-    const int *own = p.ws_unit + 2 * own_unit(b, g, own_row / p.own_rows, p);
-    const int *shr = p.ws_unit + 2 * shared_unit_of(sq[1] + group_row / p.rows_per_block, g, p);
+    // what does not depend on one another is asked for together, used or not: the
+    // sequence's place, the own unit's record, and the row that it has in `out` if whole
+    const i32x4 sq = reinterpret_cast<const i32x4 *>(p.ws_seq)[b];
+    typedef int i32x2 __attribute__((ext_vector_type(2)));
+    const i32x2 own = *reinterpret_cast<const i32x2 *>(
+        p.ws_unit + 2 * own_unit(b, g, own_row / p.own_rows, p));
+    const bf16x8 own_o = *reinterpret_cast<const bf16x8 *>(p.out + row * D + d8 * 8);
+    const float own_z = p.ws_lse2[rows + row];
+    if (i >= sq[3]) return;                         // padding: written by the main kernel
     const bool shared = sq[2] > 0;
-    const int own_first = own[0], own_last = own[1];
-    if (!shared && own_first < 0) return;
+    const int group_row = sq[0] * p.G + own_row;
+    if (!shared && own[0] < 0) return;
+    i32x2 shr = {-1, -1};
+    if (shared)
+        shr = *reinterpret_cast<const i32x2 *>(
+            p.ws_unit + 2 * shared_unit_of(sq[1] + group_row / p.rows_per_block, g, p));
 
     float M = kNegInf, den = 0.f;
     float acc[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-    auto add = [&](const uint16_t *o, float m, float l) {
-        const bf16x8 v = *reinterpret_cast<const bf16x8 *>(o + d8 * 8);
+    auto add = [&](const bf16x8 &v, float m, float l) {
         const float Mn = fmaxf(M, m);
         const float sc = (M == kNegInf) ? 0.f : __builtin_amdgcn_exp2f(M - Mn);
         const float wt = (m == kNegInf) ? 0.f : __builtin_amdgcn_exp2f(m - Mn) * l;
@@ -1723,23 +1732,21 @@ __global__ __launch_bounds__(256) void shared_join_kernel(AttnParams p) {
         for (int e = 0; e < 8; ++e) acc[e] = acc[e] * sc + wt * (float)v[e];
         M = Mn;
     };
-    auto add_unit = [&](int first, int last, int rl, int slot_rows, const uint16_t *ws_o, const float *ws_ml,
-                        const uint16_t *whole, const float *lse2) {
-        if (first < 0) {
-            add(whole + row * D, lse2[row], 1.f);
-            return;
-        }
+    auto add_pieces = [&](int first, int last, int rl, int slot_rows, const uint16_t *ws_o, const float *ws_ml) {
         #pragma unroll 4
         for (int u = first >> 1; u <= last; ++u) {
             // the first piece may sit in slot 1 of its workgroup; later ones start a share
             const size_t r = (size_t)(u == (first >> 1) ? first : u * 2) * slot_rows + rl;
             const f32x2 ml = *reinterpret_cast<const f32x2 *>(ws_ml + r * 2);
-            add(ws_o + r * D, ml[0], ml[1]);
+            add(*reinterpret_cast<const bf16x8 *>(ws_o + r * D + d8 * 8), ml[0], ml[1]);
         }
     };
-    if (shared)
-        add_unit(shr[0], shr[1], group_row % p.rows_per_block, p.rows_per_block, p.ws_o, p.ws_ml, p.ws_so, p.ws_lse2);
-    add_unit(own_first, own_last, own_row % p.own_rows, p.own_rows, p.own_o, p.own_ml, p.out, p.ws_lse2 + rows);
+    if (own[0] < 0) add(own_o, own_z, 1.f);
+    else add_pieces(own[0], own[1], own_row % p.own_rows, p.own_rows, p.own_o, p.own_ml);
+    if (shared && shr[0] < 0)
+        add(*reinterpret_cast<const bf16x8 *>(p.ws_so + row * D + d8 * 8), p.ws_lse2[row], 1.f);
+    else if (shared)
+        add_pieces(shr[0], shr[1], group_row % p.rows_per_block, p.rows_per_block, p.ws_o, p.ws_ml);
     const float inv = den > 0.f ? 1.f / den : 0.f;
     bf16x8 o;
     #pragma unroll
@@ -1803,7 +1810,6 @@ hipError_t launch_shared_d(const AttnParams &p, hipStream_t s) {
         case 1: e = go(std::integral_constant<int, 1>{}); break;
         case 2: e = go(std::integral_constant<int, 2>{}); break;
         case 3: e = go(std::integral_constant<int, 3>{}); break;
-        case 4: e = go(std::integral_constant<int, 4>{}); break;
         default: e = go(std::integral_constant<int, 0>{}); break;
     }
     if (e != hipSuccess) return e;

@@ -1,13 +1,13 @@
 // What each sequence of a batch with shared prefixes has behind the shared
-// tiles, where it has at most 64 query rows per KV head: a part of
+// tiles, where it has at most 48 query rows per KV head: a part of
 // tree_attention.hip, whose ring, tables and helpers it uses.
 //
 // A unit is one (sequence, KV head): its keys are the prefix positions behind
 // the shared tiles and then its tree nodes, one list without a gap, in tiles
 // of 8 KB of keys and 8 KB of values (32 keys of head size 128, 64 of 64). All
-// units' tiles (and one for the start of each) are laid end to end and every
-// wave takes an equal share by itself: it has 16 KB of the ring to itself,
-// loads a tile into it, and computes all RT x 16 rows of the unit on it with
+// units' tiles are laid end to end (kOwnTile places each, and one for the start
+// of a unit) and every wave takes those that begin in its equal share of the
+// places, by itself: it has 16 KB of the ring to itself, loads a tile into it, and computes all RT x 16 rows of the unit on it with
 // v_mfma_f32_16x16x32_bf16 in the layout of the narrow units above. The next
 // tile's keys are loaded once this tile's scores are taken, its values once this
 // tile's have been used, also across units; nothing is shared between waves, so
@@ -19,8 +19,8 @@
 namespace tv {
 namespace {
 
-// A real tile of a wave's share (wave-uniform). `base` is the virtual place of its
-// unit, whose tile ti sits at base + 1 + ti; from, L, nodes: of its sequence.
+// A tile of a wave's share (wave-uniform). `base` is the place of its unit, whose
+// tile ti begins at base + 1 + ti * kOwnTile; from, L, nodes: of its sequence.
 struct OwnTile {
     int b, g, ti, nt, base;
     int from, L, nodes;
@@ -91,8 +91,9 @@ __device__ __forceinline__ void own_shares(const AttnParams &p, int wid, int wav
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
     auto uni = [](int x) { return __builtin_amdgcn_readfirstlane(x); };
     const int first = uni(g_vcum[p.groups]), total = uni(g_vcum[p.groups + p.B]) - first;
-    // no share is empty, so that the pieces of a split unit sit in consecutive waves
-    waves = min(waves, total);
+    // every share is so long that a tile begins in it: the pieces of a split unit sit in
+    // consecutive waves
+    waves = min(waves, total / (kOwnTile + 1));
     if (wid >= waves) return;
     const int start = uni(first + (int)((long long)wid * total / waves));
     const int end = uni(first + (int)((long long)(wid + 1) * total / waves));
@@ -121,7 +122,7 @@ __device__ __forceinline__ void own_shares(const AttnParams &p, int wid, int wav
         if (t.ti + 1 < t.nt) {
             ++t.ti;
         } else {
-            t.base += t.nt + 1;
+            t.base += t.nt * kOwnTile + 1;
             t.ti = 0;
             if (++t.g == p.Hkv) {
                 t.g = 0;
@@ -134,7 +135,7 @@ __device__ __forceinline__ void own_shares(const AttnParams &p, int wid, int wav
                 } while (t.nt == 0);
             }
         }
-        t.ok = t.base + 1 + t.ti < end;
+        t.ok = t.base + 1 + t.ti * kOwnTile < end;
         return t;
     };
     OwnTile cur;
@@ -147,10 +148,15 @@ __device__ __forceinline__ void own_shares(const AttnParams &p, int wid, int wav
         cur.b = uni(lo);
         look_up(cur);
         const int off = start - uni(g_vcum[p.groups + cur.b]);
-        cur.g = uni(off / (cur.nt + 1));
-        cur.base = start - (off - cur.g * (cur.nt + 1));
-        cur.ti = max(start - cur.base - 1, 0);
-        cur.ok = cur.base + 1 + cur.ti < end;
+        const int per = cur.nt * kOwnTile + 1;
+        cur.g = uni(off / per);
+        cur.base = start - (off - cur.g * per);
+        cur.ti = (max(start - cur.base - 1, 0) + kOwnTile - 1) / kOwnTile;     // the first that begins here
+        cur.ok = cur.base + 1 + cur.ti * kOwnTile < end;
+        if (cur.ti == cur.nt) {                        // all of this unit's began before: the next one's first
+            cur.ti = cur.nt - 1;
+            cur = next(cur);
+        }
     }
     if (!cur.ok) return;
 

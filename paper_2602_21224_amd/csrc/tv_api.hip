@@ -112,8 +112,10 @@ AttnWorkspace attn_workspace(const AttnShape &s, int D, int max_wg) {
 }
 
 // Batches with shared prefixes run workgroups of eight waves throughout: a
-// group's rows are many. Own units of at most 64 rows are taken wave by wave
-// (tree_attention_own.h), larger ones in row blocks like the shared ones.
+// group's rows are many. Own units of at most 48 rows are taken wave by wave
+// (tree_attention_own.h), larger ones in row blocks like the shared ones: 16 sequences
+// with 32, 48 and 64 rows over 4096 shared and up to 1024 own tokens 37, 42 and 67 us
+// wave by wave, 42, 46 and 50 in row blocks.
 struct SharedShape {
     AttnShape wide;
     int own_rows, own_tiles16, own_blocks;
@@ -126,7 +128,7 @@ SharedShape shared_shape(int N, int Hq, int Hkv) {
     s.wide.rows_per_block = s.wide.waves * tv::kRowsPerWave;
     s.wide.row_blocks = (s.wide.rows + s.wide.rows_per_block - 1) / s.wide.rows_per_block;
     s.wide.tree_tiles_all = s.wide.row_blocks * ((N + tv::kKeyTile - 1) / tv::kKeyTile);   // at most
-    s.own_tiles16 = s.wide.rows <= 64 ? (s.wide.rows + 15) / 16 : 0;
+    s.own_tiles16 = s.wide.rows <= 48 ? (s.wide.rows + 15) / 16 : 0;
     s.own_rows = s.own_tiles16 ? 16 * s.own_tiles16 : s.wide.rows_per_block;
     s.own_blocks = s.own_tiles16 ? 1 : s.wide.row_blocks;
     return s;
@@ -423,17 +425,17 @@ int tree_verify_attention_shared(
     const SharedWorkspace ws = shared_workspace(s, B, N, Hq, Hkv, D, groups, max_wg);
     if (workspace_bytes < ws.total) return TV_ERR_WORKSPACE;
 
-    // the (virtual) tile count of the whole launch must fit in int32 for any kv_len (own
-    // tiles of units of few rows: half as many keys, at least)
+    // the (virtual) tile count of the whole launch must fit in int32 for any kv_len; own
+    // units of few rows count four places for 32 keys
     const long max_len = (long)max_pages * P;
-    const long blocks = 2l * B * s.wide.row_blocks + shared_blocks(s, B, groups);
-    auto tiles = [&](long len) {
+    auto tiles = [&](long len, int own) {
+        const long blocks = own * (long)B * s.own_blocks + shared_blocks(s, B, groups);
         return Hkv * (blocks * ((len + tv::kKeyTile - 1) / tv::kKeyTile + kSetupTiles) +
-                      2l * B * s.wide.tree_tiles_all);
+                      own * (long)B * s.wide.tree_tiles_all);
     };
-    if (tiles(max_len) >= (1l << 30)) return TV_ERR_SHAPE;
+    if (tiles(max_len, s.own_tiles16 ? 8 : 1) >= (1l << 30)) return TV_ERR_SHAPE;
     if (!device_ok()) return TV_ERR_DEVICE;
-    long num_wg = tiles(max_kv_len < max_len ? max_kv_len : max_len) / kMinShareTiles;
+    long num_wg = tiles(max_kv_len < max_len ? max_kv_len : max_len, 1) / kMinShareTiles;
     if (num_wg < 1) num_wg = 1;
     if (num_wg > max_wg) num_wg = max_wg;
     // the two kinds of units divide the workgroups in multiples of the XCDs, both at least one

@@ -128,6 +128,30 @@ struct EvictParams {
     int move_here;               // the selecting workgroup moves the rows itself
 };
 
+// Inclusive sums and (of numbers >= 0) maxima over the lanes of a wave, without LDS:
+// within rows of 16 lanes by shifts of 1, 2, 4 and 8, then each row's last lane onto the
+// next row, and lane 31 onto the upper half.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ int dpp_or_zero(int x) {
+    return __builtin_amdgcn_update_dpp(0, x, CTRL, ROWS, 0xF, false);
+}
+__device__ __forceinline__ int wave_prefix_sum(int x) {
+    x += dpp_or_zero<0x111, 0xF>(x);
+    x += dpp_or_zero<0x112, 0xF>(x);
+    x += dpp_or_zero<0x114, 0xF>(x);
+    x += dpp_or_zero<0x118, 0xF>(x);
+    x += dpp_or_zero<0x142, 0xA>(x);
+    return x + dpp_or_zero<0x143, 0xC>(x);
+}
+__device__ __forceinline__ int wave_prefix_max(int x) {
+    x = max(x, dpp_or_zero<0x111, 0xF>(x));
+    x = max(x, dpp_or_zero<0x112, 0xF>(x));
+    x = max(x, dpp_or_zero<0x114, 0xF>(x));
+    x = max(x, dpp_or_zero<0x118, 0xF>(x));
+    x = max(x, dpp_or_zero<0x142, 0xA>(x));
+    return max(x, dpp_or_zero<0x143, 0xC>(x));
+}
+
 // Workgroup -> logical index remap: the hardware hands consecutive workgroup
 // ids to consecutive XCDs; give every XCD one contiguous run of logical ids
 // so neighbouring work (which shares K/V rows) shares that XCD's L2.
