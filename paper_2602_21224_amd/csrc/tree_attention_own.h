@@ -351,45 +351,55 @@ __device__ __forceinline__ void own_shares(const AttnParams &p, int wid, int wav
                             st.o[rt][d0 + d], 0, 0, 0);
                 }
         });
-        // ---- the unit's (or the share's) last tile: a whole unit goes to out, a piece to a
-        // slot of this wave, normalised by its own sum: slot 0 continues a unit, slot 1 begins one
+        // ---- the unit's (or the share's) last tile. A whole unit leaves its rows, in out if there
+        // are no shared keys beside it; a piece goes to a slot of this wave, normalised by its own
+        // sum: slot 0 continues a unit, slot 1 begins one
         const bool ends = cur.ti + 1 == cur.nt;
         if (ends || !nxt.ok) {
-            const bool whole = piece_ti == 0 && ends;
+            const bool whole = piece_ti == 0 && ends, last = whole && cur.from == 0;
             const int slot = wid * 2 + (piece_ti > 0 ? 0 : 1);
             if (lane == 0) {
                 int32_t *rec = p.ws_unit + 2 * (cur.b * p.Hkv + cur.g);
                 if (piece_ti == 0) rec[0] = whole ? -1 : slot;
                 if (ends) rec[1] = wid;
             }
+            const size_t all = (size_t)p.B * p.N * p.Hq;
             #pragma unroll
             for (int rt = 0; rt < RT; ++rt) {
                 const int r = rt * 16 + i16;
                 const float l = rows_sum(st.l[rt]);
                 const float inv = l > 0.f ? 1.f / l : 0.f;
-                const bool real = r < nodes * p.G;
-                const size_t row = ((size_t)cur.b * p.N + rnode[rt]) * p.Hq + cur.g * p.G + rhead[rt];
-                uint16_t *o = whole ? p.out + row * D : p.own_o + ((size_t)slot * (RT * 16) + r) * D;
-                if (real) {
+                float unscale = 1.f, scaled = inv;
+                if (!last) {
+                    float top = 0.f;
                     #pragma unroll
-                    for (int db = 0; db < NDB; ++db) {
-                        bf16x4 v;
+                    for (int db = 0; db < NDB; ++db)
+                        #pragma unroll
+                        for (int i = 0; i < 4; ++i) top = fmaxf(top, fabsf(st.o[rt][db][i]));
+                    scaled *= part_scale(rows_max(top) * inv, unscale);
+                }
+                if (r >= nodes * p.G) continue;
+                const size_t row = ((size_t)cur.b * p.N + rnode[rt]) * p.Hq + cur.g * p.G + rhead[rt];
+                const size_t piece = (size_t)slot * (RT * 16) + r;
+                uint16_t *o = last ? p.out + row * D : whole ? p.ws_whole + (all + row) * D : p.own_o + piece * D;
+                #pragma unroll
+                for (int db = 0; db < NDB; ++db) {
+                    bf16x4 v;
+                    if (last) {
                         #pragma unroll
                         for (int i = 0; i < 4; ++i) v[i] = (__bf16)(st.o[rt][db][i] * inv);
-                        *reinterpret_cast<bf16x4 *>(o + db * 16 + 4 * g4) = v;
+                    } else {
+                        f16x4 f;
+                        #pragma unroll
+                        for (int i = 0; i < 4; ++i) f[i] = (_Float16)(st.o[rt][db][i] * scaled);
+                        v = __builtin_bit_cast(bf16x4, f);
                     }
-                    if (g4 == 0) {
-                        const float m2 = st.m[rt] * c;
-                        if (whole) {
-                            const float z = m2 + __builtin_amdgcn_logf(l);
-                            p.ws_lse2[(size_t)p.B * p.N * p.Hq + row] = z;
-                            if (p.lse) p.lse[row] = z * kLn2;
-                        } else {
-                            float *ml = p.own_ml + ((size_t)slot * (RT * 16) + r) * 2;
-                            ml[0] = st.m[rt] == kNegInf ? kNegInf : m2;
-                            ml[1] = l;
-                        }
-                    }
+                    *reinterpret_cast<bf16x4 *>(o + db * 16 + 4 * g4) = v;
+                }
+                if (g4 == 0) {
+                    const float m2 = st.m[rt] == kNegInf ? kNegInf : st.m[rt] * c;
+                    if (!last) (whole ? p.ws_row + all + row : p.own_piece + piece)[0] = f32x4{m2, l, unscale, 0.f};
+                    else if (p.lse) p.lse[row] = (m2 + __builtin_amdgcn_logf(l)) * kLn2;
                 }
             }
             fresh = true;

@@ -140,24 +140,31 @@ long shared_blocks(const SharedShape &s, int B, int groups) {
 }
 
 struct SharedWorkspace {
-    AttnWorkspace split;
-    size_t so, lse2, unit, seq, own_o, own_ml, total;       // byte offsets, and the whole
+    size_t o, piece, whole, row, unit, seq, own_o, own_piece, total;       // byte offsets, and the whole
 };
 
 SharedWorkspace shared_workspace(const SharedShape &s, int B, int N, int Hq, int Hkv, int D, int groups,
                                  int max_wg) {
-    SharedWorkspace w;
     const size_t rows = (size_t)B * N * Hq;
     const size_t units = ((size_t)B * s.own_blocks + (size_t)shared_blocks(s, B, groups)) * Hkv;
-    const size_t own = s.own_tiles16 ? (size_t)max_wg * s.wide.waves * 2 * s.own_rows : 0;   // rows of a wave's slots
-    w.split = attn_workspace(s.wide, D, max_wg);
-    w.so = w.split.o_bytes + w.split.ml_bytes;
-    w.lse2 = w.so + round_up(rows * D * sizeof(uint16_t), 256);
-    w.unit = w.lse2 + round_up(rows * 2 * sizeof(float), 256);
-    w.seq = w.unit + round_up(units * 2 * sizeof(int32_t), 256);
-    w.own_o = w.seq + round_up((size_t)B * 4 * sizeof(int32_t), 256);
-    w.own_ml = w.own_o + round_up(own * D * sizeof(uint16_t), 256);
-    w.total = w.own_ml + round_up(own * 2 * sizeof(float), 256) + 256;
+    const size_t slots = (size_t)max_wg * 2 * s.wide.rows_per_block;                        // rows of them
+    const size_t own = s.own_tiles16 ? (size_t)max_wg * s.wide.waves * 2 * s.own_rows : 0;   // of the waves'
+    SharedWorkspace w;
+    size_t at = 0;
+    auto take = [&](size_t elements, size_t bytes) {
+        const size_t from = at;
+        at += round_up(elements * bytes, 256);
+        return from;
+    };
+    w.o = take(slots * D, sizeof(uint16_t));
+    w.piece = take(slots * 4, sizeof(float));
+    w.whole = take(rows * 2 * D, sizeof(uint16_t));
+    w.row = take(rows * 2 * 4, sizeof(float));
+    w.unit = take(units * 2, sizeof(int32_t));
+    w.seq = take((size_t)B * 4, sizeof(int32_t));
+    w.own_o = take(own * D, sizeof(uint16_t));
+    w.own_piece = take(own * 4, sizeof(float));
+    w.total = at + 256;
     return w;
 }
 
@@ -451,15 +458,18 @@ int tree_verify_attention_shared(
     p.scale = scale > 0.f ? scale : 1.0f / sqrtf((float)D);
     p.scale_log2 = p.scale * 1.4426950408889634f;
     char *base = static_cast<char *>(workspace);
-    p.ws_o = reinterpret_cast<uint16_t *>(base);
-    p.ws_ml = reinterpret_cast<float *>(base + ws.split.o_bytes);
-    p.ws_so = reinterpret_cast<uint16_t *>(base + ws.so);
-    p.ws_lse2 = reinterpret_cast<float *>(base + ws.lse2);
-    p.ws_unit = reinterpret_cast<int32_t *>(base + ws.unit);
-    p.ws_seq = reinterpret_cast<int32_t *>(base + ws.seq);
+    auto halves = [&](size_t off) { return reinterpret_cast<uint16_t *>(base + off); };
+    auto ints = [&](size_t off) { return reinterpret_cast<int32_t *>(base + off); };
+    auto quads = [&](size_t off) { return reinterpret_cast<tv::f32x4 *>(base + off); };
+    p.ws_o = halves(ws.o);
+    p.ws_piece = quads(ws.piece);
+    p.ws_whole = halves(ws.whole);
+    p.ws_row = quads(ws.row);
+    p.ws_unit = ints(ws.unit);
+    p.ws_seq = ints(ws.seq);
     p.own_rows = s.own_rows; p.own_tiles16 = s.own_tiles16;
-    p.own_o = s.own_tiles16 ? reinterpret_cast<uint16_t *>(base + ws.own_o) : p.ws_o;
-    p.own_ml = s.own_tiles16 ? reinterpret_cast<float *>(base + ws.own_ml) : p.ws_ml;
+    p.own_o = s.own_tiles16 ? halves(ws.own_o) : p.ws_o;
+    p.own_piece = s.own_tiles16 ? quads(ws.own_piece) : p.ws_piece;
     p.group_start = group_start; p.shared_len = shared_len; p.groups = groups;
     p.rows_per_block = s.wide.rows_per_block;
     p.setup_tiles = kSetupTiles;

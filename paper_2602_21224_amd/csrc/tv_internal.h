@@ -85,15 +85,18 @@ struct AttnParams {
     // batches with shared prefixes only
     const int32_t *group_start, *shared_len;
     int groups;
-    uint16_t *ws_so;             // [B * N * Hq][D] bf16: rows of whole shared units (normalised)
-    float *ws_lse2;              // [2][B * N * Hq] log-sum-exp (base 2) of whole units: shared, own
+    // (ws_o: [num_wg * 2][rows_per_block][D] pieces; parts of rows are fp16 times a power
+    // of two here, with (max, sum, that factor's inverse, -) per row beside them)
+    f32x4 *ws_piece;             // [num_wg * 2][rows_per_block]
+    uint16_t *ws_whole;          // [2][B * N * Hq][D] rows of whole units: shared, own
+    f32x4 *ws_row;               // [2][B * N * Hq]
     int32_t *ws_unit;            // [units][2]: slot of the first piece (-1: whole), workgroup of the last
     int32_t *ws_seq;             // [B][4] per sequence: see build_shared_tables
     // the sequences' own units: rows of one, which may be those of ws_o's slots, or 16
     // per row tile that a wave takes by itself (own_tiles16 > 0)
     int own_rows, own_tiles16;
-    uint16_t *own_o;             // [slots][own_rows][D] bf16 pieces (normalised)
-    float *own_ml;               // [slots][own_rows][2] (max, sum)
+    uint16_t *own_o;             // [slots][own_rows][D] pieces
+    f32x4 *own_piece;            // [slots][own_rows]
 };
 
 // Launch parameters of the accumulated attention weights (all sizes in elements).
