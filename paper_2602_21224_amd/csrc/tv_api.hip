@@ -165,6 +165,8 @@ SharedWorkspace shared_workspace(const SharedShape &s, int B, int N, int Hq, int
     w.own_o = take(own * D, sizeof(uint16_t));
     w.own_piece = take(own * 4, sizeof(float));
     w.total = at + 256;
+    const size_t plain = attn_workspace(attn_shape(N, Hq, Hkv), D, max_wg).total;
+    if (w.total < plain) w.total = plain;
     return w;
 }
 
@@ -194,53 +196,12 @@ void argmax_plan(int B, int N, int V, int *segs, int *seg_len) {
     *seg_len = (int)len;
 }
 
-}  // namespace
-
-extern "C" {
-
-int tv_abi_version(void) { return TV_ABI_VERSION; }
-
-const char *tv_status_string(int status) {
-    switch (status) {
-        case TV_OK: return "ok";
-        case TV_ERR_NULL: return "a required pointer is NULL";
-        case TV_ERR_SHAPE: return "a size or count is outside the supported range";
-        case TV_ERR_ALIGN: return "a tensor pointer is not 16-byte aligned";
-        case TV_ERR_WORKSPACE: return "workspace missing or smaller than required";
-        case TV_ERR_HIP: return "a HIP runtime call or kernel launch failed";
-        case TV_ERR_DEVICE: return "the current device is not gfx950";
-        case TV_ERR_SCRATCH:
-            return "the call needs more scratch than the library's static buffer holds "
-                   "(TV_NOALLOC_SCRATCH_BYTES)";
-        default: return "unknown status";
-    }
-}
-
-size_t tv_attention_workspace_size(int B, int N, int Hq, int Hkv, int D) {
-    if (!attn_shape_ok(B, N, Hq, Hkv, D)) return 0;
-    const AttnShape s = attn_shape(N, Hq, Hkv);
-    return attn_workspace(s, D, cu_count() * kWgPerCu).total;
-}
-
-int tree_verify_attention(const uint16_t *q, const uint16_t *k_tree, const uint16_t *v_tree,
-                          const uint16_t *k_cache, const uint16_t *v_cache,
-                          const int32_t *page_table, const int32_t *kv_len, const int32_t *parent,
-                          const int32_t *num_nodes, int B, int N, int Hq, int Hkv, int D, int P,
-                          int max_pages, int num_pages, int max_kv_len, float scale, uint16_t *out,
-                          float *lse,
-                          void *workspace, size_t workspace_bytes, hipStream_t stream) {
-    if (!attn_shape_ok(B, N, Hq, Hkv, D)) return TV_ERR_SHAPE;
-    if (!pow2(P) || P > 256 || max_pages < 1 || num_pages < 1 || max_kv_len < 0)
-        return TV_ERR_SHAPE;
-    if (B == 0) return TV_OK;
-    if (!q || !k_tree || !v_tree || !k_cache || !v_cache || !page_table || !kv_len || !parent ||
-        !out || !workspace)
-        return TV_ERR_NULL;
-    if (!aligned16(q) || !aligned16(k_tree) || !aligned16(v_tree) || !aligned16(k_cache) ||
-        !aligned16(v_cache) || !aligned16(out) || !aligned16(workspace))
-        return TV_ERR_ALIGN;
-    if (!device_ok()) return TV_ERR_DEVICE;
-
+// tree_verify_attention behind its argument checks.
+int launch_attention(const uint16_t *q, const uint16_t *k_tree, const uint16_t *v_tree, const uint16_t *k_cache,
+                     const uint16_t *v_cache, const int32_t *page_table, const int32_t *kv_len,
+                     const int32_t *parent, const int32_t *num_nodes, int B, int N, int Hq, int Hkv, int D, int P,
+                     int max_pages, int num_pages, int max_kv_len, float scale, uint16_t *out, float *lse,
+                     void *workspace, size_t workspace_bytes, hipStream_t stream) {
     const AttnShape s = attn_shape(N, Hq, Hkv);
     const int max_wg = cu_count() * kWgPerCu;
     const AttnWorkspace ws = attn_workspace(s, D, max_wg);
@@ -302,6 +263,59 @@ int tree_verify_attention(const uint16_t *q, const uint16_t *k_tree, const uint1
     p.scale_log2 = sc * 1.4426950408889634f;
 
     return tv::launch_tree_attention(p, D, s.waves, stream) == hipSuccess ? TV_OK : TV_ERR_HIP;
+}
+
+
+}  // namespace
+
+extern "C" {
+
+int tv_abi_version(void) { return TV_ABI_VERSION; }
+
+const char *tv_status_string(int status) {
+    switch (status) {
+        case TV_OK: return "ok";
+        case TV_ERR_NULL: return "a required pointer is NULL";
+        case TV_ERR_SHAPE: return "a size or count is outside the supported range";
+        case TV_ERR_ALIGN: return "a tensor pointer is not 16-byte aligned";
+        case TV_ERR_WORKSPACE: return "workspace missing or smaller than required";
+        case TV_ERR_HIP: return "a HIP runtime call or kernel launch failed";
+        case TV_ERR_DEVICE: return "the current device is not gfx950";
+        case TV_ERR_SCRATCH:
+            return "the call needs more scratch than the library's static buffer holds "
+                   "(TV_NOALLOC_SCRATCH_BYTES)";
+        default: return "unknown status";
+    }
+}
+
+size_t tv_attention_workspace_size(int B, int N, int Hq, int Hkv, int D) {
+    if (!attn_shape_ok(B, N, Hq, Hkv, D)) return 0;
+    const AttnShape s = attn_shape(N, Hq, Hkv);
+    return attn_workspace(s, D, cu_count() * kWgPerCu).total;
+}
+
+int tree_verify_attention(const uint16_t *q, const uint16_t *k_tree, const uint16_t *v_tree,
+                          const uint16_t *k_cache, const uint16_t *v_cache,
+                          const int32_t *page_table, const int32_t *kv_len, const int32_t *parent,
+                          const int32_t *num_nodes, int B, int N, int Hq, int Hkv, int D, int P,
+                          int max_pages, int num_pages, int max_kv_len, float scale, uint16_t *out,
+                          float *lse,
+                          void *workspace, size_t workspace_bytes, hipStream_t stream) {
+    if (!attn_shape_ok(B, N, Hq, Hkv, D)) return TV_ERR_SHAPE;
+    if (!pow2(P) || P > 256 || max_pages < 1 || num_pages < 1 || max_kv_len < 0)
+        return TV_ERR_SHAPE;
+    if (B == 0) return TV_OK;
+    if (!q || !k_tree || !v_tree || !k_cache || !v_cache || !page_table || !kv_len || !parent ||
+        !out || !workspace)
+        return TV_ERR_NULL;
+    if (!aligned16(q) || !aligned16(k_tree) || !aligned16(v_tree) || !aligned16(k_cache) ||
+        !aligned16(v_cache) || !aligned16(out) || !aligned16(workspace))
+        return TV_ERR_ALIGN;
+    if (!device_ok()) return TV_ERR_DEVICE;
+
+    return launch_attention(q, k_tree, v_tree, k_cache, v_cache, page_table, kv_len, parent, num_nodes, B, N,
+                            Hq, Hkv, D, P, max_pages, num_pages, max_kv_len, scale, out, lse, workspace,
+                            workspace_bytes, stream);
 }
 
 size_t tv_argmax_workspace_size(int B, int N, int V) {
@@ -431,6 +445,16 @@ int tree_verify_attention_shared(
     const int max_wg = cu_count() * kWgPerCu;
     const SharedWorkspace ws = shared_workspace(s, B, N, Hq, Hkv, D, groups, max_wg);
     if (workspace_bytes < ws.total) return TV_ERR_WORKSPACE;
+    // Where every sequence's rows fill whole blocks, a group's fill no fewer together, and
+    // every block visits the shared tiles either way (the other blocks find them in the L2):
+    // the keys are taken as if nothing were shared (16 sequences x 256 rows, two groups: 75
+    // us, 89 through the tables and the joining kernel).
+    if (s.wide.rows % s.wide.rows_per_block == 0 && !num_nodes) {
+        if (!device_ok()) return TV_ERR_DEVICE;
+        return launch_attention(q, k_tree, v_tree, k_cache, v_cache, page_table, kv_len, parent, num_nodes, B,
+                                N, Hq, Hkv, D, P, max_pages, num_pages, max_kv_len, scale, out, lse, workspace,
+                                workspace_bytes, stream);
+    }
 
     // the (virtual) tile count of the whole launch must fit in int32 for any kv_len; own
     // units of few rows count four places for 32 keys
