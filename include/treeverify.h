@@ -257,6 +257,9 @@ TV_API int kv_compact_accepted(const uint16_t *k_tree, const uint16_t *v_tree, u
  *                sequence's kv_len is not used.
  *   workspace    >= tv_shared_attention_workspace_size(...) bytes, 16-byte
  *                aligned; contents on entry do not matter; clobbered.
+ * v_tree's rows of the real nodes are finite: a node that a row does not see gets
+ * weight 0 there, which does not hide an infinity or NaN (v_cache's rows are seen
+ * by every row, and may be anything).
  * A start that is not ascending counts as the largest before it, one outside
  * [0, B] is clamped. Where the pages of a group's sequences differ below
  * shared_len, results are unspecified. Calls captured into graphs that may

@@ -53,6 +53,9 @@ SHARED = [
     (3, 7, 5, 1, 64, 256, [0, 3], [1280], (0, 600), False, "forest"),        # pages longer than a tile
     (2, 3, 4, 4, 128, 16, [0, 2], [32], (0, 20), False, "forest"),           # shared lengths below a tile
     (8, 24, 8, 1, 128, 4, [0, 8], [1500], (0, 64), True, "capped"),          # one KV head
+    (6, 24, 16, 4, 128, 16, [0, 4, 6], [512, 192], (0, 150), False, "capped"),   # 96 rows: blocks of several sequences
+    (5, 16, 4, 2, 64, 16, [0, 5], [960], (100, 900), True, "forest"),        # 32 rows, long own parts
+    (9, 3, 32, 2, 128, 1, [0, 9], [333], (1, 70), False, "chain"),           # 48 rows, one-token pages
 ]
 
 
@@ -90,6 +93,45 @@ def test_shared_lengths_and_groups_change_nothing(oracle_mod, start, shared):
         w.v_cache[w.v_cache == W.BF16_NAN] = 0
     out, lse = attend(T, w, start, shared)
     check_attention(oracle_mod, w, out, lse, f"{start} {shared}")
+
+
+@pytest.mark.parametrize("power", [100, -100])
+@pytest.mark.parametrize("N", [2, 30])
+def test_parts_of_any_magnitude_are_joined(oracle_mod, power, N):
+    """Values far outside fp16's range, and a row with an infinity: what is left of the
+    two parts in the workspace is scaled per row."""
+    T = U.require_gpu()
+    w = C.shared_workload(745, B=4, N=N, Hq=8, Hkv=2, D=128, P=16, start=[0, 4], shared=[256], own=(10, 200),
+                          tree="chain", poison=False)
+    f = np.float32(2.0 ** power)
+    # no rounding: a bf16 times a power of two
+    w.v_cache = W.f32_to_bf16_bits(W.bf16_bits_to_f32(w.v_cache) * f)
+    w.v_tree = W.f32_to_bf16_bits(W.bf16_bits_to_f32(w.v_tree) * f)
+    out, lse = attend(T, w, [0, 4], [256])
+    check_attention(oracle_mod, w, out, lse, f"2^{power}")
+    w.v_cache[w.page_table[0, 0], 3, 1, 7] = 0x7F80              # an infinity that every row of KV head 1 sees
+    inf, _ = attend(T, w, [0, 4], [256])
+    a, b = U.bf16_to_f64(inf), U.bf16_to_f64(out)
+    hit = np.zeros(a.shape, bool)
+    hit[:, :, 4:, 7] = True
+    assert np.isposinf(a[hit]).all() and np.isfinite(a[~hit]).all()
+    assert np.array_equal(a[:, :, :4], b[:, :, :4])
+    if power == 100:
+        # an infinite row's parts are scaled by 2^-113: fp16 steps of 2^-24 there, for each of two parts,
+        # and the output's own rounding on both sides
+        np.testing.assert_allclose(a[~hit], b[~hit], rtol=2.0 ** -7, atol=2.0 * 2.0 ** (113 - 24))
+
+
+def test_the_largest_batch_of_groups(oracle_mod):
+    """512 sequences in 256 groups of any length, some of them empty."""
+    T = U.require_gpu()
+    rng = np.random.default_rng(8)
+    start = np.sort(np.append(rng.integers(0, 513, 255), [0, 512]))
+    shared = (rng.integers(0, 20, 256) * 16).tolist()
+    w = C.shared_workload(746, B=512, N=2, Hq=3, Hkv=1, D=64, P=16, start=start, shared=shared, own=(0, 40),
+                          tree="forest")
+    out, lse = attend(T, w, start, shared)
+    check_attention(oracle_mod, w, out, lse, "256 groups")
 
 
 def test_shared_attention_of_empty_sequences(oracle_mod):
@@ -196,6 +238,7 @@ WEIGHTS = [
     (2, 12, 5, 1, 128, 256, [900, 255], [3, 12], 64),              # a page that ends inside a tile
     (2, 8, 4, 4, 128, 2, [40, 90], [2, 5], 1000),                  # everything fixed
     (5, 6, 8, 2, 64, 4, [7, 2049, 100, 0, 31], [6, 1, 3, 2, 5], 3),
+    (2, 16, 8, 8, 128, 16, [48, 112], [16, 16], 40),               # the last slot of the table is taken
 ]
 
 
