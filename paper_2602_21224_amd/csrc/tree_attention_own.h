@@ -1,6 +1,6 @@
 // What each sequence of a batch with shared prefixes has behind the shared
 // tiles, where it has at most 48 query rows per KV head: a part of
-// tree_attention.hip, whose ring, tables and helpers it uses.
+// tree_attention_shared.hip, whose ring, tables and helpers it uses.
 //
 // A unit is one (sequence, KV head): its keys are the prefix positions behind
 // the shared tiles and then its tree nodes, one list without a gap, in tiles
@@ -8,7 +8,7 @@
 // units' tiles are laid end to end (kOwnTile places each, and one for the start
 // of a unit) and every wave takes those that begin in its equal share of the
 // places, by itself: it has 16 KB of the ring to itself, loads a tile into it, and computes all RT x 16 rows of the unit on it with
-// v_mfma_f32_16x16x32_bf16 in the layout of the narrow units above. The next
+// v_mfma_f32_16x16x32_bf16 in the layout of the narrow units (narrow_tile). The next
 // tile's keys are loaded once this tile's scores are taken, its values once this
 // tile's have been used, also across units; nothing is shared between waves, so
 // there is no barrier, and a unit that ends costs the other waves nothing. The
@@ -81,7 +81,7 @@ struct OwnState {
 
 // Wave `wid` of `waves`: its share of the own units' tiles.
 template <int D, int RT>
-__device__ __forceinline__ void own_shares(const AttnParams &p, int wid, int waves) {
+__device__ __forceinline__ void own_shares(const SharedAttnParams &p, int wid, int waves) {
     using Og = OwnGeo<D>;
     constexpr int C = Geo<D>::kChunks, RB = Geo<D>::kRowBytes;
     constexpr int NKS = D / 32, NDB = D / 16, KN = Og::kKeys, NKB = KN / 16, NST = KN / 32;

@@ -472,7 +472,7 @@ int tree_verify_attention_shared(
     // the two kinds of units divide the workgroups in multiples of the XCDs, both at least one
     if (s.own_tiles16) num_wg = num_wg < 2 * tv::kNumXcd ? 2 * tv::kNumXcd : num_wg / tv::kNumXcd * tv::kNumXcd;
 
-    tv::AttnParams p{};
+    tv::SharedAttnParams p{};
     p.q = q; p.k_tree = k_tree; p.v_tree = v_tree; p.k_cache = k_cache; p.v_cache = v_cache;
     p.page_table = page_table; p.kv_len = kv_len; p.parent = parent; p.num_nodes = num_nodes;
     p.out = out; p.lse = lse;

@@ -82,7 +82,10 @@ struct AttnParams {
     float scale_log2;            // softmax scale * log2(e)
     float scale;                 // softmax scale
     int whole_units;             // every workgroup takes one unit whole (nothing to merge)
-    // batches with shared prefixes only
+};
+
+// The same for batches with shared prefixes.
+struct SharedAttnParams : AttnParams {
     const int32_t *group_start, *shared_len;
     int groups;
     // (ws_o: [num_wg * 2][rows_per_block][D] pieces; parts of rows are fp16 times a power
@@ -216,7 +219,7 @@ hipError_t launch_kv_compact(const uint16_t *k_tree, const uint16_t *v_tree, uin
                              uint16_t *v_cache, const int32_t *page_table, const int32_t *kv_len,
                              const int32_t *accept_idx, const int32_t *accept_len, int B, int N,
                              int Hkv, int D, int P, int max_pages, int num_pages, hipStream_t s);
-hipError_t launch_shared_attention(const AttnParams &p, int head_dim, hipStream_t s);
+hipError_t launch_shared_attention(const SharedAttnParams &p, int head_dim, hipStream_t s);
 hipError_t launch_accumulate_weights(const WeightParams &p, int head_dim, hipStream_t s);
 hipError_t launch_evict(EvictParams p, hipStream_t s);
 hipError_t launch_validate(const int32_t *page_table, const int32_t *kv_len,
