@@ -53,8 +53,12 @@
 namespace tv {
 namespace {
 
-template <int D, int NW, bool SMALL, bool NARROW, bool WHOLE>
+// FINE: pieces of split units are fp16 times a power of two per row, with (max, sum,
+// that factor's inverse, -) beside them, instead of bf16 with (max, sum): what
+// tree_verify_attention_shared asks for, whose other paths keep their parts so.
+template <int D, int NW, bool SMALL, bool NARROW, bool WHOLE, bool FINE = false>
 __global__ __launch_bounds__(NW * kWave) void tree_attention_kernel(AttnParams p) {
+    static_assert(!FINE || !NARROW, "finer pieces: of wide units");
     using Gm = Geo<D>;
     using Issue = TileIssue<D, NW, SMALL>;
     constexpr int NT = NW * kWave;
@@ -432,6 +436,15 @@ __global__ __launch_bounds__(NW * kWave) void tree_attention_kernel(AttnParams p
             constexpr int kRowChunks = D / 8;                     // 16-byte chunks per row
             constexpr int kRowsPerPass = kWave / kRowChunks;
             unsigned char *wbuf = g_ring + wave_u * kRowsPerWave * kPitch;
+            [[maybe_unused]] float unscale = 1.f, scaled = inv;
+            if constexpr (FINE) {
+                float top = 0.f;
+                #pragma unroll
+                for (int dt = 0; dt < NDT; ++dt)
+                    #pragma unroll
+                    for (int r = 0; r < 16; ++r) top = fmaxf(top, fabsf(st.o[dt][r]));
+                scaled *= part_scale(halves_max(top) * inv, unscale);
+            }
             #pragma unroll
             for (int dt = 0; dt < NDT; ++dt)
                 #pragma unroll
@@ -439,6 +452,14 @@ __global__ __launch_bounds__(NW * kWave) void tree_attention_kernel(AttnParams p
                     bf16x4 v;
                     #pragma unroll
                     for (int i = 0; i < 4; ++i) v[i] = (__bf16)(st.o[dt][q4 * 4 + i] * inv);
+                    if constexpr (FINE) {
+                        if (!complete) {
+                            f16x4 f;
+                            #pragma unroll
+                            for (int i = 0; i < 4; ++i) f[i] = (_Float16)(st.o[dt][q4 * 4 + i] * scaled);
+                            v = __builtin_bit_cast(bf16x4, f);
+                        }
+                    }
                     *reinterpret_cast<bf16x4 *>(wbuf + col * kPitch + (dt * 32 + q4 * 8 + half * 4) * 2) = v;
                 }
             #pragma unroll
@@ -463,9 +484,10 @@ __global__ __launch_bounds__(NW * kWave) void tree_attention_kernel(AttnParams p
                             st.m_run * p.scale + __builtin_amdgcn_logf(l_tot) * kLn2;
                 } else {
                     const int rloc = wave_u * kRowsPerWave + col;
-                    float *pm = p.ws_ml + ((size_t)slot * p.rows_per_block + rloc) * 2;
+                    float *pm = p.ws_ml + ((size_t)slot * p.rows_per_block + rloc) * (FINE ? 4 : 2);
                     pm[0] = (st.m_run == kNegInf) ? kNegInf : st.m_run * p.scale_log2;
                     pm[1] = l_tot;
+                    if constexpr (FINE) pm[2] = unscale;
                 }
             }
         } else {
@@ -551,7 +573,7 @@ __global__ __launch_bounds__(NW * kWave) void tree_attention_kernel(AttnParams p
 // in an earlier share, the block merges a chunk of that unit's rows: one
 // thread per (row, 8 head-dim lanes), pieces combined in workgroup order with
 // an online log-sum-exp rescale (one pass, all loads of a piece independent).
-template <int D>
+template <int D, bool FINE = false>
 __global__ __launch_bounds__(256) void tree_attention_merge_kernel(AttnParams p, int stride) {
     constexpr int D8 = D / 8;
     constexpr int kRowsPerWg = 256 / D8;
@@ -578,14 +600,19 @@ __global__ __launch_bounds__(256) void tree_attention_merge_kernel(AttnParams p,
         // the first piece may sit in slot 1 of its workgroup; later ones start a share
         const int slot = u == wf ? s0 : u * 2;
         const size_t r = (size_t)slot * p.rows_per_block + rl;
-        const f32x2 ml = *reinterpret_cast<const f32x2 *>(p.ws_ml + r * 2);
+        const f32x2 ml = *reinterpret_cast<const f32x2 *>(p.ws_ml + r * (FINE ? 4 : 2));
+        [[maybe_unused]] float unscale = 1.f;
+        if constexpr (FINE) unscale = p.ws_ml[r * 4 + 2];
         const bf16x8 v = *reinterpret_cast<const bf16x8 *>(p.ws_o + r * D + d8 * 8);
         const float Mn = fmaxf(M, ml[0]);
         const float sc = (M == kNegInf) ? 0.f : __builtin_amdgcn_exp2f(M - Mn);
         const float wt = (ml[0] == kNegInf) ? 0.f : __builtin_amdgcn_exp2f(ml[0] - Mn) * ml[1];
         den = den * sc + wt;
         #pragma unroll
-        for (int i = 0; i < 8; ++i) acc[i] = acc[i] * sc + wt * (float)v[i];
+        for (int i = 0; i < 8; ++i) {
+            if constexpr (FINE) acc[i] = acc[i] * sc + wt * ((float)__builtin_bit_cast(f16x8, v)[i] * unscale);
+            else acc[i] = acc[i] * sc + wt * (float)v[i];
+        }
         M = Mn;
     }
     const int node = row / p.G;
@@ -603,8 +630,12 @@ __global__ __launch_bounds__(256) void tree_attention_merge_kernel(AttnParams p,
 // code: with the choice inside the kernel it came out up to 0.8 % slower (45 nodes of
 // head size 64 over 300-2500 keys 21.1 -> 21.3 us).
 template <int D, int NW, bool NARROW>
-hipError_t launch_main(const AttnParams &p, hipStream_t s) {
+hipError_t launch_main(const AttnParams &p, bool fine, hipStream_t s) {
     auto go = [&](auto kernel) { return launch_kernel(kernel, dim3(p.num_wg), dim3(NW * kWave), s, p); };
+    if constexpr (NW == 8 && !NARROW)
+        if (fine && !p.whole_units)
+            return p.small_pages ? go(tree_attention_kernel<D, NW, true, NARROW, false, true>)
+                                 : go(tree_attention_kernel<D, NW, false, NARROW, false, true>);
     if (p.whole_units)
         return p.small_pages ? go(tree_attention_kernel<D, NW, true, NARROW, true>)
                              : go(tree_attention_kernel<D, NW, false, NARROW, true>);
@@ -613,37 +644,37 @@ hipError_t launch_main(const AttnParams &p, hipStream_t s) {
 }
 
 template <int D, int NW>
-hipError_t launch_dn(const AttnParams &p, hipStream_t s) {
+hipError_t launch_dn(const AttnParams &p, bool fine, hipStream_t s) {
     hipError_t e;
     if constexpr (NW == 4)
-        e = p.narrow ? launch_main<D, NW, true>(p, s) : launch_main<D, NW, false>(p, s);
+        e = p.narrow ? launch_main<D, NW, true>(p, fine, s) : launch_main<D, NW, false>(p, fine, s);
     else
-        e = launch_main<D, NW, false>(p, s);
+        e = launch_main<D, NW, false>(p, fine, s);
     if (e != hipSuccess) return e;
     if (p.num_wg > 1 && !p.whole_units) {
         constexpr int kRowsPerWg = 256 / (D / 8);
         const int chunks = (p.rows_per_block + kRowsPerWg - 1) / kRowsPerWg;
         const int stride = (p.num_wg + kNumXcd - 1) / kNumXcd * kNumXcd;
-        e = launch_kernel(tree_attention_merge_kernel<D>, dim3(stride * chunks), dim3(256), s, p,
-                          stride);
+        e = launch_kernel(NW == 8 && fine ? tree_attention_merge_kernel<D, true> : tree_attention_merge_kernel<D>,
+                          dim3(stride * chunks), dim3(256), s, p, stride);
     }
     return e;
 }
 
 template <int D>
-hipError_t launch_d(const AttnParams &p, int waves, hipStream_t s) {
+hipError_t launch_d(const AttnParams &p, int waves, bool fine, hipStream_t s) {
     switch (waves) {
-        case 4: return launch_dn<D, 4>(p, s);
-        case 8: return launch_dn<D, 8>(p, s);
+        case 4: return launch_dn<D, 4>(p, fine, s);
+        case 8: return launch_dn<D, 8>(p, fine, s);
         default: return hipErrorInvalidValue;
     }
 }
 
 }  // namespace
 
-hipError_t launch_tree_attention(const AttnParams &p, int head_dim, int waves, hipStream_t s) {
-    if (head_dim == 64) return launch_d<64>(p, waves, s);
-    if (head_dim == 128) return launch_d<128>(p, waves, s);
+hipError_t launch_tree_attention(const AttnParams &p, int head_dim, int waves, bool fine, hipStream_t s) {
+    if (head_dim == 64) return launch_d<64>(p, waves, fine, s);
+    if (head_dim == 128) return launch_d<128>(p, waves, fine, s);
     return hipErrorInvalidValue;
 }
 

@@ -21,6 +21,8 @@ constexpr float kRescaleSlack = 8.f;   // keep a stale running max while new sco
 
 typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
 typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
+typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 
 template <int D>
 struct Geo {
@@ -146,6 +148,17 @@ template <int N>
 __device__ __forceinline__ void wait_vmcnt() {
     static_assert(N >= 0 && N < 64, "vmcnt is a 6-bit field");
     __builtin_amdgcn_s_waitcnt((N & 15) | (7 << 4) | (15 << 8) | ((N >> 4) << 14));
+}
+
+// Scale of a row of parts whose largest magnitude is `top`, a power of two that brings
+// it just below 2^15 of fp16's 65504, and its inverse. Rows with infinities are scaled so
+// that all finite fp32 values stay finite.
+__device__ __forceinline__ float part_scale(float top, float &unscale) {
+    int e = __builtin_amdgcn_frexp_expf(top);        // top = f 2^e, 1/2 <= f < 1; 0 for 0, inf and NaN
+    if (!(top < __builtin_huge_valf())) e = 128;
+    e = max(e, -100);
+    unscale = __builtin_amdgcn_ldexpf(1.f, e - 15);
+    return __builtin_amdgcn_ldexpf(1.f, 15 - e);
 }
 
 // Exclusive prefix sum of per-sequence tile counts into g_cum[0..B], the

@@ -30,9 +30,6 @@
 namespace tv {
 namespace {
 
-typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
-typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
-
 constexpr int NW = 8;                    // waves of a workgroup
 constexpr int NT = NW * kWave;
 
@@ -46,17 +43,6 @@ __shared__ int g_first[kMaxGroups];              // first sequence that has node
 __shared__ int g_blocks[kMaxGroups];             // row blocks of the sequences, each by itself
 __shared__ unsigned short g_gstart[kMaxGroups + 1];
 __shared__ unsigned short g_group[kMaxBatchShared];       // group of a sequence, or kMaxGroups
-
-// Scale of a row of parts whose largest magnitude is `top`, a power of two that brings
-// it just below 2^15 of fp16's 65504, and its inverse. Rows with infinities are scaled so
-// that all finite fp32 values stay finite.
-__device__ __forceinline__ float part_scale(float top, float &unscale) {
-    int e = __builtin_amdgcn_frexp_expf(top);        // top = f 2^e, 1/2 <= f < 1; 0 for 0, inf and NaN
-    if (!(top < __builtin_huge_valf())) e = 128;
-    e = max(e, -100);
-    unscale = __builtin_amdgcn_ldexpf(1.f, e - 15);
-    return __builtin_amdgcn_ldexpf(1.f, 15 - e);
-}
 
 // Query rows per KV head of group s: those of its sequences' real nodes.
 __device__ __forceinline__ int group_rows(int s, const SharedAttnParams &p) {

@@ -102,10 +102,10 @@ struct AttnWorkspace {
     size_t o_bytes, ml_bytes, desc_bytes, total;
 };
 
-AttnWorkspace attn_workspace(const AttnShape &s, int D, int max_wg) {
+AttnWorkspace attn_workspace(const AttnShape &s, int D, int max_wg, bool fine = false) {
     AttnWorkspace w;
     w.o_bytes = round_up((size_t)max_wg * 2 * s.rows_per_block * D * sizeof(uint16_t), 256);
-    w.ml_bytes = round_up((size_t)max_wg * 2 * s.rows_per_block * 2 * sizeof(float), 256);
+    w.ml_bytes = round_up((size_t)max_wg * 2 * s.rows_per_block * (fine ? 4 : 2) * sizeof(float), 256);
     w.desc_bytes = round_up((size_t)max_wg * 4 * sizeof(int32_t), 256);
     w.total = w.o_bytes + w.ml_bytes + w.desc_bytes;
     return w;
@@ -165,7 +165,7 @@ SharedWorkspace shared_workspace(const SharedShape &s, int B, int N, int Hq, int
     w.own_o = take(own * D, sizeof(uint16_t));
     w.own_piece = take(own * 4, sizeof(float));
     w.total = at + 256;
-    const size_t plain = attn_workspace(attn_shape(N, Hq, Hkv), D, max_wg).total;
+    const size_t plain = attn_workspace(attn_shape(N, Hq, Hkv), D, max_wg, true).total;
     if (w.total < plain) w.total = plain;
     return w;
 }
@@ -196,15 +196,15 @@ void argmax_plan(int B, int N, int V, int *segs, int *seg_len) {
     *seg_len = (int)len;
 }
 
-// tree_verify_attention behind its argument checks.
-int launch_attention(const uint16_t *q, const uint16_t *k_tree, const uint16_t *v_tree, const uint16_t *k_cache,
-                     const uint16_t *v_cache, const int32_t *page_table, const int32_t *kv_len,
+// tree_verify_attention behind its argument checks; `fine`: see launch_tree_attention.
+int launch_attention(bool fine, const uint16_t *q, const uint16_t *k_tree, const uint16_t *v_tree,
+                     const uint16_t *k_cache, const uint16_t *v_cache, const int32_t *page_table, const int32_t *kv_len,
                      const int32_t *parent, const int32_t *num_nodes, int B, int N, int Hq, int Hkv, int D, int P,
                      int max_pages, int num_pages, int max_kv_len, float scale, uint16_t *out, float *lse,
                      void *workspace, size_t workspace_bytes, hipStream_t stream) {
     const AttnShape s = attn_shape(N, Hq, Hkv);
     const int max_wg = cu_count() * kWgPerCu;
-    const AttnWorkspace ws = attn_workspace(s, D, max_wg);
+    const AttnWorkspace ws = attn_workspace(s, D, max_wg, fine);
     if (workspace_bytes < ws.total) return TV_ERR_WORKSPACE;
 
     // the (virtual) tile count of the whole launch must fit in int32 for any kv_len
@@ -262,7 +262,7 @@ int launch_attention(const uint16_t *q, const uint16_t *k_tree, const uint16_t *
     p.scale = sc;
     p.scale_log2 = sc * 1.4426950408889634f;
 
-    return tv::launch_tree_attention(p, D, s.waves, stream) == hipSuccess ? TV_OK : TV_ERR_HIP;
+    return tv::launch_tree_attention(p, D, s.waves, fine, stream) == hipSuccess ? TV_OK : TV_ERR_HIP;
 }
 
 
@@ -313,8 +313,8 @@ int tree_verify_attention(const uint16_t *q, const uint16_t *k_tree, const uint1
         return TV_ERR_ALIGN;
     if (!device_ok()) return TV_ERR_DEVICE;
 
-    return launch_attention(q, k_tree, v_tree, k_cache, v_cache, page_table, kv_len, parent, num_nodes, B, N,
-                            Hq, Hkv, D, P, max_pages, num_pages, max_kv_len, scale, out, lse, workspace,
+    return launch_attention(false, q, k_tree, v_tree, k_cache, v_cache, page_table, kv_len, parent, num_nodes, B,
+                            N, Hq, Hkv, D, P, max_pages, num_pages, max_kv_len, scale, out, lse, workspace,
                             workspace_bytes, stream);
 }
 
@@ -451,8 +451,8 @@ int tree_verify_attention_shared(
     // us, 89 through the tables and the joining kernel).
     if (s.wide.rows % s.wide.rows_per_block == 0 && !num_nodes) {
         if (!device_ok()) return TV_ERR_DEVICE;
-        return launch_attention(q, k_tree, v_tree, k_cache, v_cache, page_table, kv_len, parent, num_nodes, B,
-                                N, Hq, Hkv, D, P, max_pages, num_pages, max_kv_len, scale, out, lse, workspace,
+        return launch_attention(true, q, k_tree, v_tree, k_cache, v_cache, page_table, kv_len, parent, num_nodes,
+                                B, N, Hq, Hkv, D, P, max_pages, num_pages, max_kv_len, scale, out, lse, workspace,
                                 workspace_bytes, stream);
     }
 
