@@ -58,7 +58,6 @@ namespace {
 // tree_verify_attention_shared asks for, whose other paths keep their parts so.
 template <int D, int NW, bool SMALL, bool NARROW, bool WHOLE, bool FINE = false>
 __global__ __launch_bounds__(NW * kWave) void tree_attention_kernel(AttnParams p) {
-    static_assert(!FINE || !NARROW, "finer pieces: of wide units");
     using Gm = Geo<D>;
     using Issue = TileIssue<D, NW, SMALL>;
     constexpr int NT = NW * kWave;
@@ -540,11 +539,25 @@ __global__ __launch_bounds__(NW * kWave) void tree_attention_kernel(AttnParams p
                     if (ch == 0 && p.lse)
                         p.lse[((size_t)b * p.N + nd) * p.Hq + h] = M * p.scale + __builtin_amdgcn_logf(Lsum) * kLn2;
                 } else {
+                    [[maybe_unused]] float unscale = 1.f;
+                    if constexpr (FINE) {
+                        float top = 0.f;
+                        #pragma unroll
+                        for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf(acc[e]));
+                        #pragma unroll
+                        for (int off = 1; off < kCh; off <<= 1) top = fmaxf(top, __shfl_xor(top, off));
+                        const float scaled = inv * part_scale(top * inv, unscale);
+                        f16x8 f;
+                        #pragma unroll
+                        for (int e = 0; e < 8; ++e) f[e] = (_Float16)(acc[e] * scaled);
+                        o = __builtin_bit_cast(bf16x8, f);
+                    }
                     *reinterpret_cast<bf16x8 *>(p.ws_o + ((size_t)slot * p.rows_per_block + r) * D + ch * 8) = o;
                     if (ch == 0) {
-                        float *pm = p.ws_ml + ((size_t)slot * p.rows_per_block + r) * 2;
+                        float *pm = p.ws_ml + ((size_t)slot * p.rows_per_block + r) * (FINE ? 4 : 2);
                         pm[0] = (M == kNegInf) ? kNegInf : M * c;
                         pm[1] = Lsum;
+                        if constexpr (FINE) pm[2] = unscale;
                     }
                 }
             }
@@ -573,7 +586,7 @@ __global__ __launch_bounds__(NW * kWave) void tree_attention_kernel(AttnParams p
 // in an earlier share, the block merges a chunk of that unit's rows: one
 // thread per (row, 8 head-dim lanes), pieces combined in workgroup order with
 // an online log-sum-exp rescale (one pass, all loads of a piece independent).
-template <int D, bool FINE = false>
+template <int D>
 __global__ __launch_bounds__(256) void tree_attention_merge_kernel(AttnParams p, int stride) {
     constexpr int D8 = D / 8;
     constexpr int kRowsPerWg = 256 / D8;
@@ -600,20 +613,84 @@ __global__ __launch_bounds__(256) void tree_attention_merge_kernel(AttnParams p,
         // the first piece may sit in slot 1 of its workgroup; later ones start a share
         const int slot = u == wf ? s0 : u * 2;
         const size_t r = (size_t)slot * p.rows_per_block + rl;
-        const f32x2 ml = *reinterpret_cast<const f32x2 *>(p.ws_ml + r * (FINE ? 4 : 2));
-        [[maybe_unused]] float unscale = 1.f;
-        if constexpr (FINE) unscale = p.ws_ml[r * 4 + 2];
+        const f32x2 ml = *reinterpret_cast<const f32x2 *>(p.ws_ml + r * 2);
         const bf16x8 v = *reinterpret_cast<const bf16x8 *>(p.ws_o + r * D + d8 * 8);
         const float Mn = fmaxf(M, ml[0]);
         const float sc = (M == kNegInf) ? 0.f : __builtin_amdgcn_exp2f(M - Mn);
         const float wt = (ml[0] == kNegInf) ? 0.f : __builtin_amdgcn_exp2f(ml[0] - Mn) * ml[1];
         den = den * sc + wt;
         #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            if constexpr (FINE) acc[i] = acc[i] * sc + wt * ((float)__builtin_bit_cast(f16x8, v)[i] * unscale);
-            else acc[i] = acc[i] * sc + wt * (float)v[i];
-        }
+        for (int i = 0; i < 8; ++i) acc[i] = acc[i] * sc + wt * (float)v[i];
         M = Mn;
+    }
+    const int node = row / p.G;
+    const int hq = g * p.G + row % p.G;
+    const float inv = den > 0.f ? 1.f / den : 0.f;
+    bf16x8 o;
+    #pragma unroll
+    for (int i = 0; i < 8; ++i) o[i] = (__bf16)(acc[i] * inv);
+    *reinterpret_cast<bf16x8 *>(p.out + (((size_t)b * p.N + node) * p.Hq + hq) * D + d8 * 8) = o;
+    if (p.lse && d8 == 0)
+        p.lse[((size_t)b * p.N + node) * p.Hq + hq] = (M + __builtin_amdgcn_logf(den)) * kLn2;
+}
+
+// The same of fp16 pieces with four floats a row, and up to eight pieces' loads at once
+// (the last one's again behind the end): with the loop above, whose loads came out one
+// after the other here, two sequences x 26 nodes of head size 64 over 10000 keys took 36
+// us a call, 27 so; the plain pieces 23.
+template <int D>
+__global__ __launch_bounds__(256) void tree_attention_merge_fine_kernel(AttnParams p, int stride) {
+    constexpr int D8 = D / 8;
+    constexpr int kRowsPerWg = 256 / D8;
+    const int h = blockIdx.x % stride;
+    const int rchunk = blockIdx.x / stride;
+    if (h >= p.num_wg) return;
+    const int w = xcd_contiguous_id(h, p.num_wg);
+    const i32x4 d = ((const CONST_AS i32x4 *)p.ws_desc)[w];
+    const int b = d[0];
+    if (b < 0) return;
+    const int g = d[1], rb = d[2] & 0xFF, s0 = d[3];
+    const int rows_b = (d[2] >> 8) * p.G;
+    const int wf = s0 >> 1;
+
+    const int rl = rchunk * kRowsPerWg + threadIdx.x / D8;
+    const int d8 = threadIdx.x % D8;
+    const int row = rb * p.rows_per_block + rl;
+    if (rl >= p.rows_per_block || row >= rows_b) return;
+
+    float M = kNegInf, den = 0.f;
+    float acc[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    auto add = [&](auto count, int u0) {
+        constexpr int n = decltype(count)::value;
+        f32x4 ml[n];
+        f16x8 v[n];
+        #pragma unroll
+        for (int k = 0; k < n; ++k) {
+            const int u = min(u0 + k, w), slot = u == wf ? s0 : u * 2;
+            const size_t r = (size_t)slot * p.rows_per_block + rl;
+            ml[k] = *reinterpret_cast<const f32x4 *>(p.ws_ml + r * 4);
+            v[k] = *reinterpret_cast<const f16x8 *>(p.ws_o + r * D + d8 * 8);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        #pragma unroll
+        for (int k = 0; k < n; ++k) {
+            const float m = u0 + k <= w ? ml[k][0] : kNegInf;
+            const float Mn = fmaxf(M, m);
+            const float sc = (M == kNegInf) ? 0.f : __builtin_amdgcn_exp2f(M - Mn);
+            const float wt = (m == kNegInf) ? 0.f : __builtin_amdgcn_exp2f(m - Mn) * ml[k][1];
+            den = den * sc + wt;
+            #pragma unroll
+            for (int i = 0; i < 8; ++i) acc[i] = acc[i] * sc + wt * ((float)v[k][i] * ml[k][2]);
+            M = Mn;
+        }
+    };
+    if (w - wf == 1) {
+        add(std::integral_constant<int, 2>{}, wf);
+    } else {
+        for (int u = wf; u <= w; u += w - u < 4 ? 4 : 8) {
+            if (w - u < 4) add(std::integral_constant<int, 4>{}, u);
+            else add(std::integral_constant<int, 8>{}, u);
+        }
     }
     const int node = row / p.G;
     const int hq = g * p.G + row % p.G;
@@ -632,10 +709,9 @@ __global__ __launch_bounds__(256) void tree_attention_merge_kernel(AttnParams p,
 template <int D, int NW, bool NARROW>
 hipError_t launch_main(const AttnParams &p, bool fine, hipStream_t s) {
     auto go = [&](auto kernel) { return launch_kernel(kernel, dim3(p.num_wg), dim3(NW * kWave), s, p); };
-    if constexpr (NW == 8 && !NARROW)
-        if (fine && !p.whole_units)
-            return p.small_pages ? go(tree_attention_kernel<D, NW, true, NARROW, false, true>)
-                                 : go(tree_attention_kernel<D, NW, false, NARROW, false, true>);
+    if (fine && !p.whole_units)
+        return p.small_pages ? go(tree_attention_kernel<D, NW, true, NARROW, false, true>)
+                             : go(tree_attention_kernel<D, NW, false, NARROW, false, true>);
     if (p.whole_units)
         return p.small_pages ? go(tree_attention_kernel<D, NW, true, NARROW, true>)
                              : go(tree_attention_kernel<D, NW, false, NARROW, true>);
@@ -655,7 +731,7 @@ hipError_t launch_dn(const AttnParams &p, bool fine, hipStream_t s) {
         constexpr int kRowsPerWg = 256 / (D / 8);
         const int chunks = (p.rows_per_block + kRowsPerWg - 1) / kRowsPerWg;
         const int stride = (p.num_wg + kNumXcd - 1) / kNumXcd * kNumXcd;
-        e = launch_kernel(NW == 8 && fine ? tree_attention_merge_kernel<D, true> : tree_attention_merge_kernel<D>,
+        e = launch_kernel(fine ? tree_attention_merge_fine_kernel<D> : tree_attention_merge_kernel<D>,
                           dim3(stride * chunks), dim3(256), s, p, stride);
     }
     return e;

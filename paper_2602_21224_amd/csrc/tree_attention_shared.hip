@@ -12,10 +12,9 @@
 //   * How many keys are taken together is the kernel's choice: whole tiles, at
 //     most what the shortest sequence of the group has, so shared tiles need no
 //     mask and the sequences' own tiles start at a tile. Results do not depend
-//     on it beyond rounding. A group whose rows fill no fewer blocks together
+//     on it beyond rounding. A group whose rows fill hardly fewer blocks together
 //     than its sequences' blocks, each by itself, takes none: every block visits
-//     every tile once either way, and rows of one piece need no joining (16
-//     sequences x 512 rows over 16384 shared tokens 665 us shared, 611 not).
+//     every tile once either way, and rows of one piece need no joining.
 //   * Every row of such a group has two results to be joined, one per kind. A
 //     unit that one workgroup covers leaves whole normalised rows and their
 //     log-sum-exps, a split unit leaves pieces as above and a record of the
@@ -32,6 +31,7 @@ namespace {
 
 constexpr int NW = 8;                    // waves of a workgroup
 constexpr int NT = NW * kWave;
+constexpr int kJoinTiles = 4;            // of a row block's parts and their joining, in tiles
 
 // Work tables. "Virtual sequence" v < groups is the shared prefix of group v,
 // groups + b what sequence b has of its own.
@@ -139,9 +139,13 @@ __device__ void build_shared_tables(const SharedAttnParams &p, int w) {
         }
     }
     __syncthreads();
-    if (tid < p.groups)
-        g_gtiles[tid] = g_blocks[tid] > (D_OWN ? 1 : row_blocks_of(group_rows(tid, p), p))
-                            ? max(min(g_gtiles[tid], promised), 0) / KT : 0;
+    if (tid < p.groups) {
+        const int tiles = max(min(g_gtiles[tid], promised), 0) / KT;
+        const int apart = g_blocks[tid], together = row_blocks_of(group_rows(tid, p), p);
+        const bool pays = D_OWN ? apart > 1
+                                : (apart - together) * tiles > p.setup_tiles * together + kJoinTiles * apart;
+        g_gtiles[tid] = pays ? tiles : 0;
+    }
     __syncthreads();
     if (tid < kWave) {
         int carry = 0;

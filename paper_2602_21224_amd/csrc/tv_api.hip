@@ -134,6 +134,21 @@ SharedShape shared_shape(int N, int Hq, int Hkv) {
     return s;
 }
 
+// Whether the keys are taken by groups at all. That has tables to build and every row's
+// two parts to join, 5 to 10 us, so it has to save more: K/V rows that the plain launch
+// reads once per sequence (what it reads again it often finds in the caches), or row
+// blocks. us, plain and by groups: 25 MB of K/V rows in all 19.6 and 28.5 (3 sequences of 5
+// rows), 46 MB 23.2 and 25.7 (36 of 32), 51 MB 25.7 and 26.3 (4 of 4), 69 MB 28.4 and 26.0
+// (11 of 7). And of the rows of a sequence's blocks of 256 a quarter has to be empty, which
+// a group's rows fill: 208 rows 105 and 108, 232 rows 55 and 52, 427 rows 32.7 and 35.9, 775
+// rows 260 and 242, 1824 rows 467 and 569, 154 rows 62 and 46.
+bool sharing_pays(const AttnShape &s, int B, int Hkv, int D, int groups, long max_len) {
+    if (groups == 0 || groups >= B) return false;            // one sequence per group
+    if ((long)B * Hkv * D * 4 * max_len < 48l << 20) return false;
+    const long block = 8 * tv::kRowsPerWave, padded = (s.rows + block - 1) / block * block;
+    return (padded - s.rows) * 4 >= padded;
+}
+
 // Most row blocks per KV head that the groups' shared units can have together.
 long shared_blocks(const SharedShape &s, int B, int groups) {
     return ((long)B * s.wide.rows + s.wide.rows_per_block - 1) / s.wide.rows_per_block + groups;
@@ -445,17 +460,6 @@ int tree_verify_attention_shared(
     const int max_wg = cu_count() * kWgPerCu;
     const SharedWorkspace ws = shared_workspace(s, B, N, Hq, Hkv, D, groups, max_wg);
     if (workspace_bytes < ws.total) return TV_ERR_WORKSPACE;
-    // Where every sequence's rows fill whole blocks, a group's fill no fewer together, and
-    // every block visits the shared tiles either way (the other blocks find them in the L2):
-    // the keys are taken as if nothing were shared (16 sequences x 256 rows, two groups: 75
-    // us, 89 through the tables and the joining kernel).
-    if (s.wide.rows % s.wide.rows_per_block == 0 && !num_nodes) {
-        if (!device_ok()) return TV_ERR_DEVICE;
-        return launch_attention(true, q, k_tree, v_tree, k_cache, v_cache, page_table, kv_len, parent, num_nodes,
-                                B, N, Hq, Hkv, D, P, max_pages, num_pages, max_kv_len, scale, out, lse, workspace,
-                                workspace_bytes, stream);
-    }
-
     // the (virtual) tile count of the whole launch must fit in int32 for any kv_len; own
     // units of few rows count four places for 32 keys
     const long max_len = (long)max_pages * P;
@@ -466,7 +470,12 @@ int tree_verify_attention_shared(
     };
     if (tiles(max_len, s.own_tiles16 ? 8 : 1) >= (1l << 30)) return TV_ERR_SHAPE;
     if (!device_ok()) return TV_ERR_DEVICE;
-    long num_wg = tiles(max_kv_len < max_len ? max_kv_len : max_len, 1) / kMinShareTiles;
+    const long hint_len = max_kv_len < max_len ? max_kv_len : max_len;
+    if (!sharing_pays(s.wide, B, Hkv, D, groups, hint_len))
+        return launch_attention(true, q, k_tree, v_tree, k_cache, v_cache, page_table, kv_len, parent, num_nodes,
+                                B, N, Hq, Hkv, D, P, max_pages, num_pages, max_kv_len, scale, out, lse, workspace,
+                                workspace_bytes, stream);
+    long num_wg = tiles(hint_len, 1) / kMinShareTiles;
     if (num_wg < 1) num_wg = 1;
     if (num_wg > max_wg) num_wg = max_wg;
     // the two kinds of units divide the workgroups in multiples of the XCDs, both at least one

@@ -197,7 +197,7 @@ hipError_t launch_tree_build_many(const float *logits, const int32_t *root_token
                                   int B, int S, int V, int H, int k, int budget, int32_t *parent,
                                   int32_t *token, float *joint, int32_t *num_nodes,
                                   void *workspace, hipStream_t s);
-// fine (eight waves only): pieces of split units in fp16 with four floats of ws_ml each
+// fine: pieces of split units in fp16, with four floats of ws_ml each
 hipError_t launch_tree_attention(const AttnParams &p, int head_dim, int waves, bool fine, hipStream_t s);
 hipError_t launch_argmax_accept(const float *logits, const int32_t *draft, const int32_t *parent,
                                 const int32_t *num_nodes, int B, int N, int V, int segs,

@@ -15,12 +15,22 @@ pytestmark = pytest.mark.gpu
 # attention over shared prefixes
 # ---------------------------------------------------------------------------
 
-def attend(T, w, start, shared, d=None, **kw):
+def attend(T, w, start, shared, d=None, far=False, **kw):
+    """far: the page table has columns and the bound allows lengths at which keys are
+    taken by groups; without, these small batches are taken as if nothing were shared."""
     d = d or U.upload(w)
+    if far:
+        d = {**d, "page_table": far_table(w, d["page_table"])}
     i32 = lambda a: a if a is None or isinstance(a, torch.Tensor) else U.dev(np.asarray(a, np.int32))  # noqa: E731
     return T.tree_verify_attention_shared(
         d["q"], d["k_tree"], d["v_tree"], d["k_cache"], d["v_cache"], d["page_table"], d["kv_len"], d["parent"],
-        i32(start), i32(shared), max_kv_len=w.max_kv_len, num_nodes=d["num_nodes"], **kw)
+        i32(start), i32(shared), max_kv_len=1 << 24 if far else w.max_kv_len, num_nodes=d["num_nodes"], **kw)
+
+
+def far_table(w, table):
+    tokens = -(-(64 << 20) // (w.B * w.Hkv * w.D * 4))
+    more = torch.full((w.B, max(1, -(-tokens // w.P) - table.shape[1])), -1, dtype=torch.int32, device="cuda")
+    return torch.cat([table, more], 1)
 
 
 def check_attention(oracle_mod, w, out, lse, label):
@@ -56,22 +66,26 @@ SHARED = [
     (6, 24, 16, 4, 128, 16, [0, 4, 6], [512, 192], (0, 150), False, "capped"),   # 96 rows: blocks of several sequences
     (5, 16, 4, 2, 64, 16, [0, 5], [960], (100, 900), True, "forest"),        # 32 rows, long own parts
     (9, 3, 32, 2, 128, 1, [0, 9], [333], (1, 70), False, "chain"),           # 48 rows, one-token pages
+    (5, 100, 6, 2, 128, 16, [0, 2, 5], [1600, 256], (0, 200), True, "capped"),   # 300 rows, two blocks
+    (4, 140, 4, 1, 64, 16, [0, 4], [2048], (0, 300), False, "forest"),       # 560 rows, three blocks
 ]
 
 
+@pytest.mark.parametrize("far", [False, True])
 @pytest.mark.parametrize("case", range(len(SHARED)))
-def test_shared_attention(oracle_mod, case):
+def test_shared_attention(oracle_mod, case, far):
     T = U.require_gpu()
     B, N, Hq, Hkv, D, P, start, shared, own, ragged, tree = SHARED[case]
     w = C.shared_workload(700 + case, B=B, N=N, Hq=Hq, Hkv=Hkv, D=D, P=P, start=start, shared=shared, own=own,
                           ragged=ragged, tree=tree)
     print(f"case shared{case}: {SHARED[case]} nodes={w.num_nodes}", flush=True)
-    out, lse = attend(T, w, start, shared)
-    check_attention(oracle_mod, w, out, lse, f"shared{case}")
-    again, lse2 = attend(T, w, start, shared)
+    out, lse = attend(T, w, start, shared, far=far)
+    check_attention(oracle_mod, w, out, lse, f"shared{case} {far}")
+    again, lse2 = attend(T, w, start, shared, far=far)
     assert torch.equal(out.view(torch.int16), again.view(torch.int16)) and torch.equal(lse, lse2)
 
 
+@pytest.mark.parametrize("far", [False, True])
 @pytest.mark.parametrize("start,shared", [
     (None, None),                        # no groups
     ([0, 3], [0]),
@@ -82,7 +96,7 @@ def test_shared_attention(oracle_mod, case):
     ([-5, 9], [192]),                    # outside [0, B]: clamped
     ([1, 3], [-4]),
 ])
-def test_shared_lengths_and_groups_change_nothing(oracle_mod, start, shared):
+def test_shared_lengths_and_groups_change_nothing(oracle_mod, start, shared, far):
     """Whatever is promised of the sharing (as far as it is true), the function is the
     attention's."""
     T = U.require_gpu()
@@ -91,13 +105,14 @@ def test_shared_lengths_and_groups_change_nothing(oracle_mod, start, shared):
         w.kv_len[:] = [192, 150, 192]
         w.k_cache[w.k_cache == W.BF16_NAN] = 0
         w.v_cache[w.v_cache == W.BF16_NAN] = 0
-    out, lse = attend(T, w, start, shared)
+    out, lse = attend(T, w, start, shared, far=far)
     check_attention(oracle_mod, w, out, lse, f"{start} {shared}")
 
 
+@pytest.mark.parametrize("far", [False, True])
 @pytest.mark.parametrize("power", [100, -100])
 @pytest.mark.parametrize("N", [2, 30])
-def test_parts_of_any_magnitude_are_joined(oracle_mod, power, N):
+def test_parts_of_any_magnitude_are_joined(oracle_mod, power, N, far):
     """Values far outside fp16's range, and a row with an infinity: what is left of the
     two parts in the workspace is scaled per row."""
     T = U.require_gpu()
@@ -107,10 +122,10 @@ def test_parts_of_any_magnitude_are_joined(oracle_mod, power, N):
     # no rounding: a bf16 times a power of two
     w.v_cache = W.f32_to_bf16_bits(W.bf16_bits_to_f32(w.v_cache) * f)
     w.v_tree = W.f32_to_bf16_bits(W.bf16_bits_to_f32(w.v_tree) * f)
-    out, lse = attend(T, w, [0, 4], [256])
+    out, lse = attend(T, w, [0, 4], [256], far=far)
     check_attention(oracle_mod, w, out, lse, f"2^{power}")
     w.v_cache[w.page_table[0, 0], 3, 1, 7] = 0x7F80              # an infinity that every row of KV head 1 sees
-    inf, _ = attend(T, w, [0, 4], [256])
+    inf, _ = attend(T, w, [0, 4], [256], far=far)
     a, b = U.bf16_to_f64(inf), U.bf16_to_f64(out)
     hit = np.zeros(a.shape, bool)
     hit[:, :, 4:, 7] = True
@@ -122,7 +137,8 @@ def test_parts_of_any_magnitude_are_joined(oracle_mod, power, N):
         np.testing.assert_allclose(a[~hit], b[~hit], rtol=2.0 ** -7, atol=2.0 * 2.0 ** (113 - 24))
 
 
-def test_the_largest_batch_of_groups(oracle_mod):
+@pytest.mark.parametrize("far", [False, True])
+def test_the_largest_batch_of_groups(oracle_mod, far):
     """512 sequences in 256 groups of any length, some of them empty."""
     T = U.require_gpu()
     rng = np.random.default_rng(8)
@@ -130,11 +146,12 @@ def test_the_largest_batch_of_groups(oracle_mod):
     shared = (rng.integers(0, 20, 256) * 16).tolist()
     w = C.shared_workload(746, B=512, N=2, Hq=3, Hkv=1, D=64, P=16, start=start, shared=shared, own=(0, 40),
                           tree="forest")
-    out, lse = attend(T, w, start, shared)
+    out, lse = attend(T, w, start, shared, far=far)
     check_attention(oracle_mod, w, out, lse, "256 groups")
 
 
-def test_shared_attention_of_empty_sequences(oracle_mod):
+@pytest.mark.parametrize("far", [False, True])
+def test_shared_attention_of_empty_sequences(oracle_mod, far):
     """A group whose first sequence has no nodes (its length and pages hold anything),
     and one where none has."""
     T = U.require_gpu()
@@ -149,7 +166,7 @@ def test_shared_attention_of_empty_sequences(oracle_mod):
     ref = W.Workload(**{**w.__dict__, "page_table": w.page_table.copy(), "kv_len": w.kv_len.copy()})
     w.page_table[0], w.page_table[3] = -9, 1 << 30
     w.kv_len[0], w.kv_len[3] = 3, -2
-    out, lse = attend(T, w, [0, 3, 5], [128, 64])
+    out, lse = attend(T, w, [0, 3, 5], [128, 64], far=far)
     check_attention(oracle_mod, ref, out, lse, "empty")
 
 
@@ -161,13 +178,14 @@ def test_shared_attention_equals_the_plain_one_without_groups():
     assert np.abs(U.bf16_to_f64(a) - b).max() <= 2.0 ** -6 and np.abs(za.cpu().numpy() - zb).max() <= 1e-4
 
 
-def test_shared_attention_needs_no_lse_and_no_clean_workspace(oracle_mod):
+@pytest.mark.parametrize("far", [False, True])
+def test_shared_attention_needs_no_lse_and_no_clean_workspace(oracle_mod, far):
     T = U.require_gpu()
     w = C.shared_workload(732, B=4, N=12, Hq=8, Hkv=8, D=128, P=16, start=[0, 4], shared=[320], own=(0, 200))
-    out, lse = attend(T, w, [0, 4], [320])
+    out, lse = attend(T, w, [0, 4], [320], far=far)
     need = T.shared_attention_workspace_size(w.B, w.N, w.Hq, w.Hkv, w.D, 1)
     ws = torch.full((need,), 0xFF, dtype=torch.uint8, device="cuda")
-    again, none = attend(T, w, [0, 4], [320], workspace=ws, want_lse=False)
+    again, none = attend(T, w, [0, 4], [320], far=far, workspace=ws, want_lse=False)
     assert none is None and torch.equal(out.view(torch.int16), again.view(torch.int16))
 
 
@@ -424,13 +442,14 @@ def test_rows_of_pages_out_of_range_stay(oracle_mod):
 # streams, graphs, and a loop of them all
 # ---------------------------------------------------------------------------
 
-def test_calls_on_other_streams():
+@pytest.mark.parametrize("far", [False, True])
+def test_calls_on_other_streams(far):
     """Two calls at once, each on its own stream with its own workspace."""
     T = U.require_gpu()
     w = C.shared_workload(940, B=4, N=16, Hq=16, Hkv=4, D=128, P=16, start=[0, 4], shared=[512], own=(0, 300))
     s = C.cache_state(941, B=3, Hkv=4, D=64, P=16, lens=[900, 700, 40])
     d, e = U.upload(w), upload_state(s)
-    want, wz = attend(T, w, [0, 4], [512], d)
+    want, wz = attend(T, w, [0, 4], [512], d, far)
     copy = lambda: {**e, "k_cache": e["k_cache"].clone(), "v_cache": e["v_cache"].clone(),  # noqa: E731
                     "weight": e["weight"].clone(), "position": e["position"].clone()}
     ref = copy()
@@ -438,9 +457,13 @@ def test_calls_on_other_streams():
     two = [copy(), copy()]
     # inputs live until the other streams are done with them
     start, shared = U.dev(np.array([0, 4], np.int32)), U.dev(np.array([512], np.int32))
+    d["page_table"] = far_table(w, d["page_table"]) if far else d["page_table"]
     torch.cuda.synchronize()
     streams = [torch.cuda.Stream(), torch.cuda.Stream()]
-    outs = [attend(T, w, start, shared, d, stream=st) for st in streams]
+    hint = 1 << 24 if far else w.max_kv_len
+    outs = [T.tree_verify_attention_shared(d["q"], d["k_tree"], d["v_tree"], d["k_cache"], d["v_cache"],
+                                           d["page_table"], d["kv_len"], d["parent"], start, shared,
+                                           max_kv_len=hint, num_nodes=d["num_nodes"], stream=st) for st in streams]
     kepts = [evict(T, s, x, 256, 30, stream=st) for x, st in zip(two, streams)]
     torch.cuda.synchronize()
     for (o, z), x, k in zip(outs, two, kepts):
@@ -449,13 +472,15 @@ def test_calls_on_other_streams():
         assert torch.equal(x["k_cache"].view(torch.int16), ref["k_cache"].view(torch.int16))
 
 
-def test_a_captured_step_replays():
+@pytest.mark.parametrize("far", [False, True])
+def test_a_captured_step_replays(far):
     """Attention, weights and eviction in one graph, replayed on new inputs with eager
     work between the replays."""
     T = U.require_gpu()
     w = C.shared_workload(950, B=3, N=8, Hq=8, Hkv=2, D=128, P=16, start=[0, 3], shared=[192], own=(0, 120),
                           tree="chain", poison=False)
     d = U.upload(w)
+    at, hint = (far_table(w, d["page_table"]), 1 << 24) if far else (d["page_table"], w.max_kv_len)
     slots = (3, 2, w.page_table.shape[1] * 16)
     gs, sl = U.dev(np.array([0, 3], np.int32)), U.dev(np.array([192], np.int32))
     alen, idx = U.dev(np.array([3, 1, 8], np.int32)), torch.arange(8, dtype=torch.int32, device="cuda").repeat(3, 1)
@@ -472,8 +497,8 @@ def test_a_captured_step_replays():
         kc.copy_(d["k_cache"])
         vc.copy_(d["v_cache"])
         w1.zero_(), w2.zero_(), p2.zero_()
-        T.tree_verify_attention_shared(d["q"], d["k_tree"], d["v_tree"], kc, vc, d["page_table"], d["kv_len"],
-                                       d["parent"], gs, sl, max_kv_len=w.max_kv_len, out=out, lse=lse, workspace=ws)
+        T.tree_verify_attention_shared(d["q"], d["k_tree"], d["v_tree"], kc, vc, at, d["kv_len"],
+                                       d["parent"], gs, sl, max_kv_len=hint, out=out, lse=lse, workspace=ws)
         T.kv_compact_accepted(d["k_tree"], d["v_tree"], kc, vc, d["page_table"], d["kv_len"], idx, alen)
         T.kv_accumulate_weights(d["q"], lse, kc, d["page_table"], d["kv_len"], idx, alen, weight, position,
                                 d["kv_len"], max_kv_len=w.max_kv_len, weight_out=w1)
@@ -501,7 +526,8 @@ def test_a_captured_step_replays():
         assert all(torch.equal(a, b) for a, b in zip(got, seen())), k
 
 
-def test_a_serving_loop_with_a_shared_prompt_and_a_budget(oracle_mod):
+@pytest.mark.parametrize("far", [False, True])
+def test_a_serving_loop_with_a_shared_prompt_and_a_budget(oracle_mod, far):
     """Several steps of verification over one cache: attention over the shared prompt,
     acceptance, compaction, weights, eviction of what each sequence has of its own,
     against the oracle run on the same states."""
@@ -534,8 +560,9 @@ def test_a_serving_loop_with_a_shared_prompt_and_a_budget(oracle_mod):
                     logits[b, i, draft[b, i + 1]] += 20
         dl, ds, dpar = U.dev(lens), U.dev(seen), U.dev(parent)
         gq, gk, gv = U.dev_bf16(q), U.dev_bf16(kt), U.dev_bf16(vt)
-        out, lse = T.tree_verify_attention_shared(gq, gk, gv, dk, dv, dt, dl, dpar, gs, sl,
-                                                  max_kv_len=int(lens.max()))
+        w = W.Workload("loop", B, N, Hq, Hkv, D, P, 9, q, kt, vt, kc, vc, table, lens, parent, draft, None)
+        at, hint = (far_table(w, dt), 1 << 24) if far else (dt, int(lens.max()))
+        out, lse = T.tree_verify_attention_shared(gq, gk, gv, dk, dv, at, dl, dpar, gs, sl, max_kv_len=hint)
         _, alen, idx, _ = T.tree_argmax_accept(U.dev(logits), U.dev(draft), dpar)
         T.kv_compact_accepted(gk, gv, dk, dv, dt, dl, idx, alen)
         T.kv_accumulate_weights(gq, lse, dk, dt, dl, idx, alen, dw, dp, ds, max_kv_len=int(lens.max()), fixed_len=df)
@@ -545,7 +572,6 @@ def test_a_serving_loop_with_a_shared_prompt_and_a_budget(oracle_mod):
         *_, kept = T.kv_evict(dw, dp, dk, dv, dt, dl, ds, max_kv_len=top, budget=budget, recent=8, fixed_len=df)
         torch.cuda.synchronize()
 
-        w = W.Workload("loop", B, N, Hq, Hkv, D, P, 9, q, kt, vt, kc, vc, table, lens, parent, draft, None)
         check_attention(oracle_mod, w, out, lse, f"step {step}")
         al, ai = alen.cpu().numpy(), idx.cpu().numpy()
         kc, vc = oracle_mod.kv_compact(kt, vt, kc, vc, table, lens, ai, al)
