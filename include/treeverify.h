@@ -244,7 +244,10 @@ TV_API int kv_compact_accepted(const uint16_t *k_tree, const uint16_t *v_tree, u
  * all query rows of the group instead of once per sequence. What is computed
  * is tree_verify_attention's function of the same arguments (§2.1, §7.1: its
  * declaration above gives formulas, layouts and limits); which keys are taken
- * together changes roundings only.
+ * together changes roundings only. That is chosen by the sizes: where reading
+ * shared rows once saves less than joining the parts costs (few K/V bytes, or
+ * query rows of a sequence and KV head that nearly fill blocks of 256), the
+ * batch runs as if nothing were shared.
  *
  *   groups       number of groups, 0 <= groups <= 256; with 0 the two arrays
  *                may be NULL and every sequence is attended by itself
@@ -264,7 +267,8 @@ TV_API int kv_compact_accepted(const uint16_t *k_tree, const uint16_t *v_tree, u
  * [0, B] is clamped. Where the pages of a group's sequences differ below
  * shared_len, results are unspecified. Calls captured into graphs that may
  * run at the same time need workspaces of their own.
- * Supported: as tree_verify_attention, with 0 <= B <= 512.
+ * Supported: as tree_verify_attention, with 0 <= B <= 512 and
+ * B * N * Hq * D <= 2^34.
  * ------------------------------------------------------------------------ */
 TV_API size_t tv_shared_attention_workspace_size(int B, int N, int Hq, int Hkv, int D, int groups);
 

@@ -23,6 +23,12 @@
 // sources lie past the kept length and destinations below it, so no move reads
 // what another wrote, and only rows that have to move do. A second kernel moves
 // them with the whole chip; where there can be few, the first does.
+//
+// Kernel times: 4 sequences x 8 KV heads from 32768 slots to 8192, 27 us of selection (one
+// workgroup's passes over its registers; 32 CUs read 8 MB) and 43-45 us of moves (195 MB
+// in and out, 4.4 TB/s); 16 x 8 heads of 1900-2311 slots to 2048 11.6 us in one
+// kernel; 8 heads of 128 slots 7 us, a chain of barriers. A selection that re-read its
+// weights for every 8-bit digit and moved its rows itself took 447, 48 and 34.
 #include "tv_internal.h"
 
 namespace tv {

@@ -17,6 +17,13 @@
 // rows need (place of the query, log-sum-exp, last visible key) into LDS. The
 // sums run over the rows in order and over l / 16 at the end: fixed, without
 // atomics.
+//
+// Kernel times: 4 sequences x 8 KV heads of 32768 keys of 128, paths of up to 12 nodes x 4
+// heads, 60-63 us (277 MB, 4.4-4.6 TB/s; a large copy reads and writes 4.8); 16 sequences
+// of 1024-4096 keys 21-29 us (87 MB at their mean length), where one workgroup's wait for
+// page ids, then keys, then stores is a good part of the call; 8 heads of 128 keys 4 us.
+// A kernel with one thread per key took 296, 168 and 12; the same tiles with the keys
+// asked for one block at a time 76 and 31.
 #include "tv_internal.h"
 
 namespace tv {

@@ -7,13 +7,17 @@
 // of 8 KB of keys and 8 KB of values (32 keys of head size 128, 64 of 64). All
 // units' tiles are laid end to end (kOwnTile places each, and one for the start
 // of a unit) and every wave takes those that begin in its equal share of the
-// places, by itself: it has 16 KB of the ring to itself, loads a tile into it, and computes all RT x 16 rows of the unit on it with
-// v_mfma_f32_16x16x32_bf16 in the layout of the narrow units (narrow_tile). The next
-// tile's keys are loaded once this tile's scores are taken, its values once this
-// tile's have been used, also across units; nothing is shared between waves, so
-// there is no barrier, and a unit that ends costs the other waves nothing. The
-// eight waves keep up to 128 KB in flight per CU, which bounds the kernel by the
-// stream of K and V.
+// places, by itself: it has 16 KB of the ring to itself, loads a tile into it, and
+// computes all RT x 16 rows of the unit on it with v_mfma_f32_16x16x32_bf16 in the
+// layout of the narrow units (narrow_tile). The next tile's keys are loaded once
+// this tile's scores are taken, its values once this tile's have been used, also
+// across units; nothing is shared between waves, so there is no barrier, and a
+// unit that ends costs the other waves nothing. The eight waves keep up to 128 KB
+// in flight per CU, which bounds the kernel by the stream of K and V.
+//
+// Against row blocks for the own units too, us per call: decoding 64 sequences (own
+// keys 16-512 behind 4096 shared ones) 54 and 35, 12-token trees of 16 sequences with
+// 32 KV heads 74 and 48; from 64 rows on the row blocks are ahead (67 and 50).
 #pragma once
 
 namespace tv {

@@ -24,6 +24,12 @@
 //     the output itself): parts are fp16 with a power of two per row instead,
 //     half a step 2^-11 of them, for the same bytes (in fp32 a batch of 16
 //     sequences x 12 rows x 32 heads took 53 us instead of 47).
+//
+// Kernel times, attention and joining: decoding 64 sequences x 32 heads over 4096 shared
+// tokens and up to 512 of their own 27 + 7 us (plain call 145-180; 87 MB without
+// repetition, 18 us of a large copy), 16 sequences x 12 nodes x 32 KV heads over 1024 shared
+// and up to 1024 own tokens 37-46 + 8 us (plain 85; 157 MB, 33 us). Fill and drain, the joining
+// launch and the shares' own unevenness are what is left.
 #include "tree_attention_common.h"
 
 namespace tv {

@@ -469,6 +469,7 @@ int tree_verify_attention_shared(
                       own * (long)B * s.wide.tree_tiles_all);
     };
     if (tiles(max_len, s.own_tiles16 ? 8 : 1) >= (1l << 30)) return TV_ERR_SHAPE;
+    if ((long)B * N * Hq * D > (1l << 34)) return TV_ERR_SHAPE;   // the joining kernel's threads, 8 values each
     if (!device_ok()) return TV_ERR_DEVICE;
     const long hint_len = max_kv_len < max_len ? max_kv_len : max_len;
     if (!sharing_pays(s.wide, B, Hkv, D, groups, hint_len))
