@@ -431,10 +431,14 @@ int kv_compact_accepted(const uint16_t *k_tree, const uint16_t *v_tree, uint16_t
     return e == hipSuccess ? TV_OK : TV_ERR_HIP;
 }
 
+static bool shared_shape_ok(int B, int N, int Hq, int Hkv, int D, int groups) {
+    return attn_shape_ok(B, N, Hq, Hkv, D) && B <= tv::kMaxBatchShared && groups >= 0 &&
+           groups <= tv::kMaxGroups &&
+           (long)B * N * Hq * D <= (1l << 34);          // the joining kernel's threads, 8 values each
+}
+
 size_t tv_shared_attention_workspace_size(int B, int N, int Hq, int Hkv, int D, int groups) {
-    if (!attn_shape_ok(B, N, Hq, Hkv, D) || B > tv::kMaxBatchShared || groups < 0 ||
-        groups > tv::kMaxGroups)
-        return 0;
+    if (!shared_shape_ok(B, N, Hq, Hkv, D, groups)) return 0;
     return shared_workspace(shared_shape(N, Hq, Hkv), B, N, Hq, Hkv, D, groups, cu_count() * kWgPerCu).total;
 }
 
@@ -445,9 +449,9 @@ int tree_verify_attention_shared(
     const int32_t *shared_len, int groups, int B, int N, int Hq, int Hkv, int D, int P,
     int max_pages, int num_pages, int max_kv_len, float scale, uint16_t *out, float *lse,
     void *workspace, size_t workspace_bytes, hipStream_t stream) {
-    if (!attn_shape_ok(B, N, Hq, Hkv, D) || B > tv::kMaxBatchShared) return TV_ERR_SHAPE;
+    if (!shared_shape_ok(B, N, Hq, Hkv, D, groups)) return TV_ERR_SHAPE;
     if (!pow2(P) || P > 256 || max_pages < 1 || num_pages < 1 || max_kv_len < 0 ||
-        (long)max_pages * P > INT32_MAX || groups < 0 || groups > tv::kMaxGroups)
+        (long)max_pages * P > INT32_MAX)
         return TV_ERR_SHAPE;
     if (B == 0) return TV_OK;
     if (!q || !k_tree || !v_tree || !k_cache || !v_cache || !page_table || !kv_len || !parent ||
@@ -469,7 +473,6 @@ int tree_verify_attention_shared(
                       own * (long)B * s.wide.tree_tiles_all);
     };
     if (tiles(max_len, s.own_tiles16 ? 8 : 1) >= (1l << 30)) return TV_ERR_SHAPE;
-    if ((long)B * N * Hq * D > (1l << 34)) return TV_ERR_SHAPE;   // the joining kernel's threads, 8 values each
     if (!device_ok()) return TV_ERR_DEVICE;
     const long hint_len = max_kv_len < max_len ? max_kv_len : max_len;
     if (!sharing_pays(s.wide, B, Hkv, D, groups, hint_len))

@@ -42,6 +42,9 @@ def test_shared_attention_argument_checks(lib):
     assert shared(lib, v_cache=ODD) == -3 and shared(lib, out=ODD) == -3
     need = lib.tv_shared_attention_workspace_size(2, 8, 8, 2, 128, 1)
     assert need > 0 and shared(lib, ws_bytes=need - 1) == -4
+    many = dict(B=512, N=256, Hq=1025, Hkv=1025, ws_bytes=1 << 62)        # more than 2^34 output values
+    assert shared(lib, **many) == -2 and shared(lib, **{**many, "Hq": 1024, "Hkv": 1024, "q": NULL}) == -1
+    assert lib.tv_shared_attention_workspace_size(512, 256, 1025, 1025, 128, 1) == 0
     # well-formed on a machine without a GPU: stops at the device check, launches nothing
     assert shared(lib) in (-4, -6)
     assert shared(lib, groups=0, group_start=NULL, shared_len=NULL) in (-4, -6)
