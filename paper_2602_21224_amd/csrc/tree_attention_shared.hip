@@ -37,7 +37,6 @@ namespace {
 
 constexpr int NW = 8;                    // waves of a workgroup
 constexpr int NT = NW * kWave;
-constexpr int kJoinTiles = 4;            // of a row block's parts and their joining, in tiles
 
 // Work tables. "Virtual sequence" v < groups is the shared prefix of group v,
 // groups + b what sequence b has of its own.

@@ -112,10 +112,12 @@ AttnWorkspace attn_workspace(const AttnShape &s, int D, int max_wg, bool fine = 
 }
 
 // Batches with shared prefixes run workgroups of eight waves throughout: a
-// group's rows are many. Own units of at most 48 rows are taken wave by wave
+// group's rows are many. Own units of at most kOwnRows rows are taken wave by wave
 // (tree_attention_own.h), larger ones in row blocks like the shared ones: 16 sequences
 // with 32, 48 and 64 rows over 4096 shared and up to 1024 own tokens 37, 42 and 67 us
 // wave by wave, 42, 46 and 50 in row blocks.
+constexpr int kOwnRows = 48;
+
 struct SharedShape {
     AttnShape wide;
     int own_rows, own_tiles16, own_blocks;
@@ -128,7 +130,7 @@ SharedShape shared_shape(int N, int Hq, int Hkv) {
     s.wide.rows_per_block = s.wide.waves * tv::kRowsPerWave;
     s.wide.row_blocks = (s.wide.rows + s.wide.rows_per_block - 1) / s.wide.rows_per_block;
     s.wide.tree_tiles_all = s.wide.row_blocks * ((N + tv::kKeyTile - 1) / tv::kKeyTile);   // at most
-    s.own_tiles16 = s.wide.rows <= 48 ? (s.wide.rows + 15) / 16 : 0;
+    s.own_tiles16 = s.wide.rows <= kOwnRows ? (s.wide.rows + 15) / 16 : 0;
     s.own_rows = s.own_tiles16 ? 16 * s.own_tiles16 : s.wide.rows_per_block;
     s.own_blocks = s.own_tiles16 ? 1 : s.wide.row_blocks;
     return s;
@@ -141,12 +143,17 @@ SharedShape shared_shape(int N, int Hq, int Hkv) {
 // rows), 46 MB 23.2 and 25.7 (36 of 32), 51 MB 25.7 and 26.3 (4 of 4), 69 MB 28.4 and 26.0
 // (11 of 7). And of the rows of a sequence's blocks of 256 a quarter has to be empty, which
 // a group's rows fill: 208 rows 105 and 108, 232 rows 55 and 52, 427 rows 32.7 and 35.9, 775
-// rows 260 and 242, 1824 rows 467 and 569, 154 rows 62 and 46.
+// rows 260 and 242, 1824 rows 467 and 569, 154 rows 62 and 46. Row blocks of eight waves
+// also have to save more tiles than they cost, by the count that the kernel makes of each
+// group: 29 sequences of 273 rows over 154 tokens 118 and 133.
 bool sharing_pays(const AttnShape &s, int B, int Hkv, int D, int groups, long max_len) {
     if (groups == 0 || groups >= B) return false;            // one sequence per group
     if ((long)B * Hkv * D * 4 * max_len < 48l << 20) return false;
     const long block = 8 * tv::kRowsPerWave, padded = (s.rows + block - 1) / block * block;
-    return (padded - s.rows) * 4 >= padded;
+    if ((padded - s.rows) * 4 < padded) return false;
+    if (s.rows <= kOwnRows) return true;
+    const long apart = B * (padded / block), together = (B * (long)s.rows + block - 1) / block;
+    return (apart - together) * (max_len / tv::kKeyTile) > kSetupTiles * together + tv::kJoinTiles * apart;
 }
 
 // Most row blocks per KV head that the groups' shared units can have together.

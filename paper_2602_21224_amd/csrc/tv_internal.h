@@ -28,6 +28,7 @@ constexpr int kMaxNodes = 256;
 constexpr int kMaxBatchAttn = 1024;
 constexpr int kMaxBatchShared = 512; // shared-prefix attention: the LDS tables of sequences and groups
 constexpr int kMaxGroups = 256;
+constexpr int kJoinTiles = 4;    // cost of a row block's parts and their joining, in tiles
 constexpr int kTbMaxK = 16;          // tree builder: largest branch number
 constexpr int kTbMaxSteps = 16;      // tree builder: most speculative steps
 
