@@ -138,17 +138,18 @@ SharedShape shared_shape(int N, int Hq, int Hkv) {
 
 // Whether the keys are taken by groups at all. That has tables to build and every row's
 // two parts to join, 5 to 10 us, so it has to save more: K/V rows that the plain launch
-// reads once per sequence (what it reads again it often finds in the caches), or row
-// blocks. us, plain and by groups: 25 MB of K/V rows in all 19.6 and 28.5 (3 sequences of 5
-// rows), 46 MB 23.2 and 25.7 (36 of 32), 51 MB 25.7 and 26.3 (4 of 4), 69 MB 28.4 and 26.0
-// (11 of 7). And of the rows of a sequence's blocks of 256 a quarter has to be empty, which
-// a group's rows fill: 208 rows 105 and 108, 232 rows 55 and 52, 427 rows 32.7 and 35.9, 775
-// rows 260 and 242, 1824 rows 467 and 569, 154 rows 62 and 46. Row blocks of eight waves
-// also have to save more tiles than they cost, by the count that the kernel makes of each
-// group: 29 sequences of 273 rows over 154 tokens 118 and 133.
+// reads again (which it often finds in the caches), or row blocks. us, plain and by groups:
+// at most 19 MB of K/V rows saved 24.4 and 29.9 (3 sequences of 3 rows, two groups), 17 MB
+// 19.6 and 28.5 (3 of 5 rows), 30 MB 23.2 and 25.7 (36 of 32, 12 groups), 34 MB 33.4 and 28.3
+// (4 of 56, two groups), 39 MB 25.7 and 26.3 (4 of 4), 44 MB 26.9 and 18.8 (36 of 8, two
+// groups), 63 MB 28.4 and 26.0 (11 of 7). And of the rows of a sequence's blocks of 256 a
+// quarter has to be empty, which a group's rows fill: 208 rows 105 and 108, 232 rows 55 and
+// 52, 427 rows 32.7 and 35.9, 775 rows 260 and 242, 1824 rows 467 and 569, 154 rows 62 and
+// 46. Row blocks of eight waves also have to save more tiles than they cost, by the count
+// that the kernel makes of each group: 29 sequences of 273 rows over 154 tokens 118 and 133.
 bool sharing_pays(const AttnShape &s, int B, int Hkv, int D, int groups, long max_len) {
     if (groups == 0 || groups >= B) return false;            // one sequence per group
-    if ((long)B * Hkv * D * 4 * max_len < 48l << 20) return false;
+    if ((long)(B - groups) * Hkv * D * 4 * max_len < 32l << 20) return false;
     const long block = 8 * tv::kRowsPerWave, padded = (s.rows + block - 1) / block * block;
     if ((padded - s.rows) * 4 < padded) return false;
     if (s.rows <= kOwnRows) return true;
