@@ -28,7 +28,7 @@ def attend(T, w, start, shared, d=None, far=False, **kw):
 
 
 def far_table(w, table):
-    tokens = -(-(64 << 20) // (w.B * w.Hkv * w.D * 4))
+    tokens = -(-(256 << 20) // (w.B * w.Hkv * w.D * 4))
     more = torch.full((w.B, max(1, -(-tokens // w.P) - table.shape[1])), -1, dtype=torch.int32, device="cuda")
     return torch.cat([table, more], 1)
 
