@@ -432,14 +432,23 @@ struct TileIssue {
     }
 
     // Direct-to-LDS loads of this wave's blocks of one K (or V) tile into ring
-    // stage `stage`.
+    // stage `stage`. A key of a block behind its last existing one reads the block's
+    // first row of K, whose scores are replaced. Its weight in V is 0, and 0 times an
+    // infinity of a cached row is NaN, so there it reads tree node 0's row, in a load of
+    // its own: a selected address cost the eight-wave kernels spills, and a load more than
+    // the waits count makes them wait for more, never for less. (With pages shorter than
+    // a block only tree tiles come here.)
     __device__ __forceinline__ void issue(const Blocks &bl, bool is_v, int stage, int wave_u) const {
         unsigned char *dst = g_ring + stage * Gm::kStageBytes + (is_v ? Gm::kTileBytes : 0);
         #pragma unroll
         for (int i = 0; i < LPT; ++i) {
-            const char *addr = (is_v ? bl.v[i] : bl.k[i]) + ((kib < bl.nv[i] ? row_off : 0u) + chunk_off[i]);
-            __builtin_amdgcn_global_load_lds((const GLOBAL_AS void *)addr,
-                                             (LDS_AS void *)(dst + (wave_u * LPT + i) * 1024), 16, 0, 0);
+            const bool in = kib < bl.nv[i];
+            const char *addr = (is_v ? bl.v[i] : bl.k[i]) + ((in ? row_off : 0u) + chunk_off[i]);
+            LDS_AS void *to = (LDS_AS void *)(dst + (wave_u * LPT + i) * 1024);
+            if (SMALL || !is_v || in)
+                __builtin_amdgcn_global_load_lds((const GLOBAL_AS void *)addr, to, 16, 0, 0);
+            else
+                __builtin_amdgcn_global_load_lds((const GLOBAL_AS void *)(vt_g + chunk_off[i]), to, 16, 0, 0);
         }
     }
 
