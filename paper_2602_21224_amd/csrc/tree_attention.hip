@@ -674,7 +674,8 @@ __global__ __launch_bounds__(256) void tree_attention_merge_fine_kernel(AttnPara
         __builtin_amdgcn_sched_barrier(0);
         #pragma unroll
         for (int k = 0; k < n; ++k) {
-            const float m = u0 + k <= w ? ml[k][0] : kNegInf;
+            if (u0 + k > w) break;                   // a repeat: left out, 0 times an infinity is NaN
+            const float m = ml[k][0];
             const float Mn = fmaxf(M, m);
             const float sc = (M == kNegInf) ? 0.f : __builtin_amdgcn_exp2f(M - Mn);
             const float wt = (m == kNegInf) ? 0.f : __builtin_amdgcn_exp2f(m - Mn) * ml[k][1];

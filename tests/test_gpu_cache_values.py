@@ -49,3 +49,14 @@ def test_an_infinity_ahead_of_missing_keys_of_own_row_blocks_stays_one():
     out, _ = attend(T, w, [0, 6], [1024], far=True)
     check_special(out[4])
     assert np.isfinite(U.bf16_to_f64(out)[[0, 1, 2, 3, 5]]).all()
+
+
+@pytest.mark.parametrize("N,D", [(2, 128), (12, 64), (40, 128)])
+@pytest.mark.parametrize("length", [200, 330, 390, 450, 520, 580, 777, 900, 1100, 1500, 2300])
+def test_an_infinity_in_the_last_piece_stays_one(length, N, D):
+    """Units split into two to twenty pieces, the last of which holds the last cached row."""
+    T = U.require_gpu()
+    w = C.shared_workload(1020, B=1, N=N, Hq=8, Hkv=2, D=D, P=16, start=[0, 1], shared=[0], own=(length, length),
+                          tree="chain", poison=False)
+    special(w, 0, length - 1)
+    check_special(attend(T, w, None, None)[0])
