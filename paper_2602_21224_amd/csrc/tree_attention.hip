@@ -437,12 +437,15 @@ __global__ __launch_bounds__(NW * kWave) void tree_attention_kernel(AttnParams p
             unsigned char *wbuf = g_ring + wave_u * kRowsPerWave * kPitch;
             [[maybe_unused]] float unscale = 1.f, scaled = inv;
             if constexpr (FINE) {
-                float top = 0.f;
-                #pragma unroll
-                for (int dt = 0; dt < NDT; ++dt)
-                    #pragma unroll
-                    for (int r = 0; r < 16; ++r) top = fmaxf(top, fabsf(st.o[dt][r]));
-                scaled *= part_scale(halves_max(top) * inv, unscale);
+                const float top = row_top(
+                    [&](auto take) {
+                        #pragma unroll
+                        for (int dt = 0; dt < NDT; ++dt)
+                            #pragma unroll
+                            for (int r = 0; r < 16; ++r) take(st.o[dt][r]);
+                    },
+                    halves_max);
+                scaled *= part_scale(top * inv, unscale);
             }
             #pragma unroll
             for (int dt = 0; dt < NDT; ++dt)
@@ -541,11 +544,16 @@ __global__ __launch_bounds__(NW * kWave) void tree_attention_kernel(AttnParams p
                 } else {
                     [[maybe_unused]] float unscale = 1.f;
                     if constexpr (FINE) {
-                        float top = 0.f;
-                        #pragma unroll
-                        for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf(acc[e]));
-                        #pragma unroll
-                        for (int off = 1; off < kCh; off <<= 1) top = fmaxf(top, __shfl_xor(top, off));
+                        const float top = row_top(
+                            [&](auto take) {
+                                #pragma unroll
+                                for (int e = 0; e < 8; ++e) take(acc[e]);
+                            },
+                            [&](float x) {
+                                #pragma unroll
+                                for (int off = 1; off < kCh; off <<= 1) x = fmaxf(x, __shfl_xor(x, off));
+                                return x;
+                            });
                         const float scaled = inv * part_scale(top * inv, unscale);
                         f16x8 f;
                         #pragma unroll

@@ -150,12 +150,30 @@ __device__ __forceinline__ void wait_vmcnt() {
     __builtin_amdgcn_s_waitcnt((N & 15) | (7 << 4) | (15 << 8) | ((N >> 4) << 14));
 }
 
-// Scale of a row of parts whose largest magnitude is `top`, a power of two that brings
-// it just below 2^15 of fp16's 65504, and its inverse. Rows with infinities are scaled so
-// that all finite fp32 values stay finite.
+// Largest finite magnitude of a row of parts (0 if there is none). `each` hands the lane's
+// values to a function, `over` takes the maximum over the lanes that hold the row. An
+// infinity does not set the scale, which would flush the columns beside it to 0: it stays one
+// in fp16 whatever it is multiplied by. NaN passes both maxima by.
+template <typename Each, typename Over>
+__device__ __forceinline__ float row_top(Each each, Over over) {
+    float top = 0.f;
+    each([&](float x) { top = fmaxf(top, fabsf(x)); });
+    top = over(top);
+    if (__any(top == __builtin_huge_valf())) {       // rare: the second look is skipped without
+        top = 0.f;
+        each([&](float x) {
+            const float a = fabsf(x);
+            top = fmaxf(top, a < __builtin_huge_valf() ? a : 0.f);
+        });
+        top = over(top);
+    }
+    return top;
+}
+
+// Scale of a row of parts whose largest finite magnitude is `top`, a power of two that
+// brings it just below 2^15 of fp16's 65504, and its inverse.
 __device__ __forceinline__ float part_scale(float top, float &unscale) {
-    int e = __builtin_amdgcn_frexp_expf(top);        // top = f 2^e, 1/2 <= f < 1; 0 for 0, inf and NaN
-    if (!(top < __builtin_huge_valf())) e = 128;
+    int e = __builtin_amdgcn_frexp_expf(top);        // top = f 2^e, 1/2 <= f < 1; 0 for 0
     e = max(e, -100);
     unscale = __builtin_amdgcn_ldexpf(1.f, e - 15);
     return __builtin_amdgcn_ldexpf(1.f, 15 - e);

@@ -375,12 +375,15 @@ __device__ __forceinline__ void own_shares(const SharedAttnParams &p, int wid, i
                 const float inv = l > 0.f ? 1.f / l : 0.f;
                 float unscale = 1.f, scaled = inv;
                 if (!last) {
-                    float top = 0.f;
-                    #pragma unroll
-                    for (int db = 0; db < NDB; ++db)
-                        #pragma unroll
-                        for (int i = 0; i < 4; ++i) top = fmaxf(top, fabsf(st.o[rt][db][i]));
-                    scaled *= part_scale(rows_max(top) * inv, unscale);
+                    const float top = row_top(
+                        [&](auto take) {
+                            #pragma unroll
+                            for (int db = 0; db < NDB; ++db)
+                                #pragma unroll
+                                for (int i = 0; i < 4; ++i) take(st.o[rt][db][i]);
+                        },
+                        rows_max);
+                    scaled *= part_scale(top * inv, unscale);
                 }
                 if (r >= nodes * p.G) continue;
                 const size_t row = ((size_t)cur.b * p.N + rnode[rt]) * p.Hq + cur.g * p.G + rhead[rt];

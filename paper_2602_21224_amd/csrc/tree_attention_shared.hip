@@ -533,12 +533,15 @@ __global__ __launch_bounds__(NT) void shared_attention_kernel(SharedAttnParams p
         unsigned char *wbuf = g_ring + wave_u * kRowsPerWave * kPitch;
         float unscale = 1.f, scaled = inv;
         if (!last) {
-            float top = 0.f;
-            #pragma unroll
-            for (int dt = 0; dt < NDT; ++dt)
-                #pragma unroll
-                for (int r = 0; r < 16; ++r) top = fmaxf(top, fabsf(st.o[dt][r]));
-            scaled *= part_scale(halves_max(top) * inv, unscale);
+            const float top = row_top(
+                [&](auto take) {
+                    #pragma unroll
+                    for (int dt = 0; dt < NDT; ++dt)
+                        #pragma unroll
+                        for (int r = 0; r < 16; ++r) take(st.o[dt][r]);
+                },
+                halves_max);
+            scaled *= part_scale(top * inv, unscale);
         }
         #pragma unroll
         for (int dt = 0; dt < NDT; ++dt)

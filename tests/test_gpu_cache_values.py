@@ -4,6 +4,7 @@ import numpy as np
 import pytest
 import torch
 
+from paper_2602_21224_amd import workloads as W
 from tests import cache_util as C
 from tests import gpu_util as U
 from tests.test_gpu_cache import attend
@@ -60,3 +61,60 @@ def test_an_infinity_in_the_last_piece_stays_one(length, N, D):
                           tree="chain", poison=False)
     special(w, 0, length - 1)
     check_special(attend(T, w, None, None)[0])
+
+
+def check_beside(oracle_mod, w, out, seqs, label):
+    """`w` without the three special values, which KV head 1 of the sequences `seqs` has in
+    columns 7, 9 and 11. Every other column is what it is without them: the attention's
+    bound, and half a subnormal step of the fp16 parts, 2^-25 where a row's largest
+    magnitude is 2^14 at least."""
+    want, _, bound = C.attention_bounds(oracle_mod, w)
+    mag = 2.0 ** 8 * bound                         # at least 2 sum p |v|
+    bound = bound + 2.0 ** -39 * mag.max(-1, keepdims=True)
+    got = U.bf16_to_f64(out)
+    G = w.Hq // w.Hkv
+    hit = np.zeros(got.shape[:3], bool)
+    hit[seqs, :, G:2 * G] = True
+    assert np.isposinf(got[hit][:, 7]).all() and np.isneginf(got[hit][:, 9]).all(), label
+    assert np.isnan(got[hit][:, 11]).all(), label
+    finite = np.ones(got.shape, bool)
+    finite[np.ix_(seqs, range(w.N), range(G, 2 * G), (7, 9, 11))] = False
+    err = np.where(finite, np.abs(np.where(finite, got, 0) - want), 0)
+    print(f"[{label}] of its bound {(err / bound).max():.2f}", flush=True)
+    assert (err <= bound).all(), label
+
+
+def scale_values(w, power):
+    f = np.float32(2.0 ** power)                   # exact: bf16 times a power of two
+    w.v_cache = W.f32_to_bf16_bits(W.bf16_bits_to_f32(w.v_cache) * f)
+    w.v_tree = W.f32_to_bf16_bits(W.bf16_bits_to_f32(w.v_tree) * f)
+
+
+BESIDE = [
+    # B, N, Hq, Hkv, D, P, shared, own, far
+    (4, 2, 8, 2, 128, 16, 256, (10, 200), True),       # own units of 16 rows
+    (3, 12, 8, 2, 64, 1, 320, (70, 400), True),        # of 48 rows, one-token pages
+    (6, 24, 8, 2, 128, 16, 1024, (100, 300), True),    # shared and own row blocks
+    (4, 2, 8, 2, 128, 16, 256, (10, 200), False),      # split units of 16 rows, nothing shared
+    (4, 30, 8, 2, 64, 16, 256, (10, 200), False),      # of 128 rows
+    (2, 64, 8, 2, 128, 16, 512, (300, 700), False),    # of 256 rows
+]
+
+
+@pytest.mark.parametrize("power", [0, 100, -100])
+@pytest.mark.parametrize("case", range(len(BESIDE)))
+def test_columns_beside_an_infinity_keep_their_values(oracle_mod, case, power):
+    """+inf, -inf and NaN in a shared row, which every sequence sees, and in the last of
+    one sequence's own rows."""
+    T = U.require_gpu()
+    B, N, Hq, Hkv, D, P, shared, own, far = BESIDE[case]
+    w = C.shared_workload(1000 + case, B=B, N=N, Hq=Hq, Hkv=Hkv, D=D, P=P, start=[0, B], shared=[shared], own=own,
+                          tree="capped", poison=False)
+    scale_values(w, power)
+    clean = w.v_cache.copy()
+    for where, b, t, seqs in (("shared", 0, 3, list(range(B))), ("own", 1, int(w.kv_len[1]) - 1, [1])):
+        w.v_cache = clean.copy()
+        special(w, b, t)
+        out, _ = attend(T, w, [0, B], [shared], far=far)
+        w.v_cache = clean
+        check_beside(oracle_mod, w, out, seqs, f"beside{case} 2^{power} {where}")
