@@ -267,8 +267,8 @@ TV_API int kv_compact_accepted(const uint16_t *k_tree, const uint16_t *v_tree, u
  * [0, B] is clamped. Where the pages of a group's sequences differ below
  * shared_len, results are unspecified. Calls captured into graphs that may
  * run at the same time need workspaces of their own.
- * Supported: as tree_verify_attention, with 0 <= B <= 512 and
- * B * N * Hq * D <= 2^34.
+ * Supported: as tree_verify_attention, with 0 <= B <= 512,
+ * B * N * Hq * D <= 2^34 and max_pages * P < 2^31.
  * ------------------------------------------------------------------------ */
 TV_API size_t tv_shared_attention_workspace_size(int B, int N, int Hq, int Hkv, int D, int groups);
 

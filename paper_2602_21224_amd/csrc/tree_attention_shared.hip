@@ -62,14 +62,11 @@ __device__ __forceinline__ int shared_tiles_of(int b) {
 
 template <int D>
 struct OwnGeo {
-    static constexpr int kKeys = 4096 / D;             // per tile
+    static constexpr int kKeys = own_keys(D);          // per tile
     static constexpr int kLoads = 8;                   // 1 KB loads of K (and of V) per tile
     static constexpr int kKeysPerLoad = 512 / D;
     static constexpr int kHalfBytes = 8192;            // of K, and of V
 };
-
-// Places (virtual tiles) of an own tile; a unit has one more in front, for its start.
-constexpr int kOwnTile = 2;
 
 // Time of a (virtual) tile of the shared units, which is bound by its products, in
 // places of own units, whose tiles are bound by their loads and, of several row tiles,

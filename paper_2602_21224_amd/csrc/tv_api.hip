@@ -219,6 +219,23 @@ void argmax_plan(int B, int N, int V, int *segs, int *seg_len) {
     *seg_len = (int)len;
 }
 
+// Virtual tiles of a launch of tree_verify_attention over prefixes of `len` tokens. They
+// are counted in int32 on the device: fewer than kMaxTiles for any kv_len.
+constexpr long kMaxTiles = 1l << 30;
+
+long attn_tiles(const AttnShape &s, int B, int Hkv, long len) {
+    return (long)B * Hkv *
+           ((long)s.row_blocks * ((len + tv::kKeyTile - 1) / tv::kKeyTile + kSetupTiles) + s.tree_tiles_all);
+}
+
+// The same of a launch that takes keys by groups; small own units count places (tree_attention_own.h).
+long shared_places(const SharedShape &s, int B, int N, int Hkv, int D, int groups, long len) {
+    const long prefix = (len + tv::kKeyTile - 1) / tv::kKeyTile + kSetupTiles, keys = tv::own_keys(D);
+    const long own = s.own_tiles16 ? (len + N + keys - 1) / keys * tv::kOwnTile + 1
+                                   : s.own_blocks * prefix + s.wide.tree_tiles_all;
+    return Hkv * (shared_blocks(s, B, groups) * prefix + B * own);
+}
+
 // tree_verify_attention behind its argument checks; `fine`: see launch_tree_attention.
 int launch_attention(bool fine, const uint16_t *q, const uint16_t *k_tree, const uint16_t *v_tree,
                      const uint16_t *k_cache, const uint16_t *v_cache, const int32_t *page_table, const int32_t *kv_len,
@@ -230,18 +247,11 @@ int launch_attention(bool fine, const uint16_t *q, const uint16_t *k_tree, const
     const AttnWorkspace ws = attn_workspace(s, D, max_wg, fine);
     if (workspace_bytes < ws.total) return TV_ERR_WORKSPACE;
 
-    // the (virtual) tile count of the whole launch must fit in int32 for any kv_len
     const long max_len = (long)max_pages * P;
-    const long worst = (long)B * Hkv *
-                       ((long)s.row_blocks * ((max_len + tv::kKeyTile - 1) / tv::kKeyTile + kSetupTiles) +
-                        s.tree_tiles_all);
-    if (worst >= (1l << 30)) return TV_ERR_SHAPE;
+    if (attn_tiles(s, B, Hkv, max_len) >= kMaxTiles) return TV_ERR_SHAPE;
 
     const long hint_len = max_kv_len < max_len ? max_kv_len : max_len;
-    const long est = (long)B * Hkv *
-                     ((long)s.row_blocks * ((hint_len + tv::kKeyTile - 1) / tv::kKeyTile + kSetupTiles) +
-                      s.tree_tiles_all);
-    long num_wg = est / kMinShareTiles;
+    long num_wg = attn_tiles(s, B, Hkv, hint_len) / kMinShareTiles;
     if (num_wg < 1) num_wg = 1;
     if (num_wg > max_wg) num_wg = max_wg;
     // Short units are not worth splitting: one workgroup per unit saves the merge
@@ -472,22 +482,20 @@ int tree_verify_attention_shared(
     const int max_wg = cu_count() * kWgPerCu;
     const SharedWorkspace ws = shared_workspace(s, B, N, Hq, Hkv, D, groups, max_wg);
     if (workspace_bytes < ws.total) return TV_ERR_WORKSPACE;
-    // the (virtual) tile count of the whole launch must fit in int32 for any kv_len; own
-    // units of few rows count four places for 32 keys
-    const long max_len = (long)max_pages * P;
-    auto tiles = [&](long len, int own) {
-        const long blocks = own * (long)B * s.own_blocks + shared_blocks(s, B, groups);
-        return Hkv * (blocks * ((len + tv::kKeyTile - 1) / tv::kKeyTile + kSetupTiles) +
-                      own * (long)B * s.wide.tree_tiles_all);
-    };
-    if (tiles(max_len, s.own_tiles16 ? 8 : 1) >= (1l << 30)) return TV_ERR_SHAPE;
+    // Tables that hold longer prefixes than keys taken by groups can be counted for take the
+    // plain launch, too: what it accepts is accepted.
+    const long max_len = (long)max_pages * P, hint_len = max_kv_len < max_len ? max_kv_len : max_len;
+    const bool grouped = shared_places(s, B, N, Hkv, D, groups, max_len) < kMaxTiles &&
+                         sharing_pays(s.wide, B, Hkv, D, groups, hint_len);
+    if (!grouped && attn_tiles(attn_shape(N, Hq, Hkv), B, Hkv, max_len) >= kMaxTiles) return TV_ERR_SHAPE;
     if (!device_ok()) return TV_ERR_DEVICE;
-    const long hint_len = max_kv_len < max_len ? max_kv_len : max_len;
-    if (!sharing_pays(s.wide, B, Hkv, D, groups, hint_len))
+    if (!grouped)
         return launch_attention(true, q, k_tree, v_tree, k_cache, v_cache, page_table, kv_len, parent, num_nodes,
                                 B, N, Hq, Hkv, D, P, max_pages, num_pages, max_kv_len, scale, out, lse, workspace,
                                 workspace_bytes, stream);
-    long num_wg = tiles(hint_len, 1) / kMinShareTiles;
+    const long blocks = (long)B * s.own_blocks + shared_blocks(s, B, groups);
+    long num_wg = Hkv * (blocks * ((hint_len + tv::kKeyTile - 1) / tv::kKeyTile + kSetupTiles) +
+                         (long)B * s.wide.tree_tiles_all) / kMinShareTiles;
     if (num_wg < 1) num_wg = 1;
     if (num_wg > max_wg) num_wg = max_wg;
     // the two kinds of units divide the workgroups in multiples of the XCDs, both at least one

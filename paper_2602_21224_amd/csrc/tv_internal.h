@@ -29,6 +29,8 @@ constexpr int kMaxBatchAttn = 1024;
 constexpr int kMaxBatchShared = 512; // shared-prefix attention: the LDS tables of sequences and groups
 constexpr int kMaxGroups = 256;
 constexpr int kJoinTiles = 4;    // cost of a row block's parts and their joining, in tiles
+constexpr int kOwnTile = 2;      // places (virtual tiles) of an own tile; a unit has one more in front, for its start
+constexpr int own_keys(int head_dim) { return 4096 / head_dim; }   // keys of an own tile
 constexpr int kTbMaxK = 16;          // tree builder: largest branch number
 constexpr int kTbMaxSteps = 16;      // tree builder: most speculative steps
 
