@@ -118,3 +118,36 @@ def test_columns_beside_an_infinity_keep_their_values(oracle_mod, case, power):
         out, _ = attend(T, w, [0, B], [shared], far=far)
         w.v_cache = clean
         check_beside(oracle_mod, w, out, seqs, f"beside{case} 2^{power} {where}")
+
+
+@pytest.mark.parametrize("case", range(len(BESIDE)))
+def test_parts_of_rows_keep_eleven_bits(case):
+    """Queries of zeros weigh every key by exactly 1, so nothing is rounded but the parts
+    and the output, whose true values are means of values 1 + k 2^-7 < 1.125: half a step
+    of the output, 2^-8; half a step of the parts, whose weights' sum is 1, 2^-11 of them in
+    fp16; fp32 sums, half a step 2^-24 a key, and some for the joining. Parts in bf16 (half a
+    step 2^-8) put one value in 6 to 2000 outside this bound."""
+    T = U.require_gpu()
+    B, N, Hq, Hkv, D, P, shared, own, far = BESIDE[case]
+    w = C.shared_workload(1040 + case, B=B, N=N, Hq=Hq, Hkv=Hkv, D=D, P=P, start=[0, B], shared=[shared], own=own,
+                          tree="chain", poison=False)
+    rng = np.random.default_rng(case)
+    for name in ("v_cache", "v_tree"):
+        values = rng.integers(0, 16, getattr(w, name).shape).astype(np.float32) / 128 + 1
+        setattr(w, name, W.f32_to_bf16_bits(values))
+    w.q[:] = 0
+    out, lse = attend(T, w, [0, B], [shared], far=far)
+    got, z = U.bf16_to_f64(out), lse.cpu().numpy().astype(np.float64)
+    tree = np.cumsum(W.bf16_bits_to_f32(w.v_tree).astype(np.float64), 1)       # a chain: node i sees 0 .. i
+    worst = 0.0
+    for b, L in enumerate(w.kv_len):
+        t = np.arange(L)
+        cached = W.bf16_bits_to_f32(w.v_cache[w.page_table[b, t // P], t % P]).astype(np.float64).sum(0)
+        n = L + 1.0 + np.arange(N)
+        mean = ((cached + tree[b]) / n[:, None, None]).repeat(Hq // Hkv, 1)
+        bound = 2.0 ** -8 + 1.125 * (2.0 ** -11 + (L + N + 64) * 2.0 ** -24)
+        worst = max(worst, np.abs(got[b] - mean).max() / bound)
+        # log n, of sums of up to n ones and powers of 2
+        assert (np.abs(z[b] - np.log(n)[:, None]) <= 2.0 ** -24 * (L + N + 64)).all()
+    print(f"[parts{case}] of the bound {worst:.2f}", flush=True)
+    assert worst <= 1
