@@ -86,7 +86,8 @@ enum tv_status {
     TV_ERR_WORKSPACE = -4,   /* workspace missing or smaller than required      */
     TV_ERR_HIP = -5,         /* a HIP runtime call or kernel launch failed      */
     TV_ERR_DEVICE = -6,      /* the current device is not gfx950                */
-    TV_ERR_SCRATCH = -7      /* more scratch needed than the static buffer holds */
+    TV_ERR_SCRATCH = -7,     /* more scratch needed than the static buffer holds */
+    TV_ERR_OVERLAP = -8      /* an output overlaps an input that it may not overlap */
 };
 
 /* TV_ABI_VERSION of the built library. */
@@ -353,7 +354,8 @@ TV_API int kv_accumulate_weights(const uint16_t *q, const float *lse, const uint
  *   seen, fixed_len   [B] int32 as for kv_accumulate_weights (fixed_len or NULL)
  *   kept_len          [B] int32 out: the caller's next kv_len. kv_len and
  *                     page_table are not modified; pages past kept_len are the
- *                     caller's again. May not overlap kv_len.
+ *                     caller's again. May not overlap kv_len, seen or
+ *                     fixed_len (TV_ERR_OVERLAP).
  *   workspace         >= tv_evict_workspace_size(B, Hkv, max_pages, P) bytes,
  *                     16-byte aligned; contents on entry do not matter.
  * A row whose page id is out of range is not moved (contract violation).

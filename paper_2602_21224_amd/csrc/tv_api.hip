@@ -69,6 +69,11 @@ int cu_count() {
 }
 
 bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+// Whether two int32 arrays of n elements share any.
+bool overlap(const int32_t *a, const int32_t *b, long n) {
+    const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+    return (x < y ? y - x : x - y) < (uintptr_t)n * sizeof(int32_t);
+}
 bool pow2(int x) { return x > 0 && (x & (x - 1)) == 0; }
 size_t round_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
 
@@ -317,6 +322,7 @@ const char *tv_status_string(int status) {
         case TV_ERR_SCRATCH:
             return "the call needs more scratch than the library's static buffer holds "
                    "(TV_NOALLOC_SCRATCH_BYTES)";
+        case TV_ERR_OVERLAP: return "an output array overlaps an input that it may not overlap";
         default: return "unknown status";
     }
 }
@@ -589,6 +595,9 @@ int kv_evict(const float *weight, const int32_t *position, uint16_t *k_cache, ui
     if (!aligned16(k_cache) || !aligned16(v_cache) || !aligned16(workspace)) return TV_ERR_ALIGN;
     if (workspace_bytes < tv_evict_workspace_size(B, Hkv, max_pages, P)) return TV_ERR_WORKSPACE;
     if (!device_ok()) return TV_ERR_DEVICE;
+    // one workgroup of a sequence writes its kept length while others read these
+    if (overlap(kept_len, kv_len, B) || overlap(kept_len, seen, B) || overlap(kept_len, fixed_len, B))
+        return TV_ERR_OVERLAP;
     tv::EvictParams p{};
     p.weight = weight; p.position = position; p.page_table = page_table; p.kv_len = kv_len;
     p.seen = seen; p.fixed_len = fixed_len; p.k_cache = k_cache; p.v_cache = v_cache;
