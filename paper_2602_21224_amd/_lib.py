@@ -307,10 +307,20 @@ def _want_on(dev, t, name, dtypes, shape=None):
 _current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
 
 
+def _own(dev, stream, shape, dtype):
+    """A tensor of the wrapper's own for a call on `stream`: from that stream's memory, whose
+    earlier uses the call is behind (the current stream's may still be running)."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=dev)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=dev)
+
+
 def _call(what, dev, stream, own, *args):
     """Call the C entry point on device `dev` (made current for the call where it is not)
-    and on `stream`. `own`: tensors that the wrapper allocated, which the caching allocator
-    must not hand out again before another stream than the current one is done with them."""
+    and on `stream`. `own`: results that the wrapper allocated for another stream than the
+    current one, where the caller goes on with them: the caching allocator does not hand
+    them out again before the current stream is done with them."""
     fn = getattr(_lib or load(), what)
     if dev != _current_device():
         with torch.cuda.device(dev):
@@ -321,7 +331,7 @@ def _call(what, dev, stream, own, *args):
         st = fn(*args, _stream(stream))
     if stream is not None:
         for t in own:
-            t.record_stream(stream)
+            t.record_stream(torch.cuda.current_stream(dev))
     if st != 0:
         _check(st, what)
 
@@ -362,18 +372,17 @@ def tree_verify_attention_shared(q, k_tree, v_tree, k_cache, v_cache, page_table
         _want_on(dev, shared_len, "shared_len", _I32, (groups,))
     own = []
     if out is None:
-        out = torch.empty((B, N, Hq, D), dtype=torch.bfloat16, device=q.device)
+        out = _own(dev, stream, (B, N, Hq, D), torch.bfloat16)
         own.append(out)
     _want_on(dev, out, "out", _BF16, (B, N, Hq, D))
     if lse is None and want_lse:
-        lse = torch.empty((B, N, Hq), dtype=torch.float32, device=q.device)
+        lse = _own(dev, stream, (B, N, Hq), torch.float32)
         own.append(lse)
     if lse is not None:
         _want_on(dev, lse, "lse", _F32, (B, N, Hq))
     if workspace is None:
         need = shared_attention_workspace_size(B, N, Hq, Hkv, D, groups)
-        workspace = torch.empty(max(need, 16), dtype=torch.uint8, device=q.device)
-        own.append(workspace)
+        workspace = _own(dev, stream, max(need, 16), torch.uint8)
     _want_on(dev, workspace, "workspace", _U8)
     _call("tree_verify_attention_shared", dev, stream, own,
           _ptr(q), _ptr(k_tree), _ptr(v_tree), _ptr(k_cache), _ptr(v_cache), _ptr(page_table),
@@ -451,15 +460,14 @@ def kv_evict(weight, position, k_cache, v_cache, page_table, kv_len, seen, *, ma
     _want_on(dev, position_out, "position_out", _I32, slots)
     own = []
     if kept_len is None:
-        kept_len = torch.empty((B,), dtype=torch.int32, device=k_cache.device)
+        kept_len = _own(dev, stream, (B,), torch.int32)
         own.append(kept_len)
     _want_on(dev, kept_len, "kept_len", _I32, (B,))
     if kept_len.data_ptr() == kv_len.data_ptr() and B > 0:
         raise ValueError("kept_len must not be kv_len itself")
     if workspace is None:
         need = evict_workspace_size(B, Hkv, max_pages, P)
-        workspace = torch.empty(max(need, 16), dtype=torch.uint8, device=k_cache.device)
-        own.append(workspace)
+        workspace = _own(dev, stream, max(need, 16), torch.uint8)
     _want_on(dev, workspace, "workspace", _U8)
     _call("kv_evict", dev, stream, own,
           _ptr(weight), _ptr(position), _ptr(k_cache), _ptr(v_cache), _ptr(page_table),
