@@ -245,13 +245,23 @@ TV_API int kv_compact_accepted(const uint16_t *k_tree, const uint16_t *v_tree, u
  * all query rows of the group instead of once per sequence. What is computed
  * is tree_verify_attention's function of the same arguments (§2.1, §7.1: its
  * declaration above gives formulas, layouts and limits); which keys are taken
- * together changes roundings only. That is chosen by the sizes: where reading
- * shared rows once saves less than joining the parts costs (few K/V bytes, or
- * query rows of a sequence and KV head that nearly fill blocks of 256), the
- * batch runs as if nothing were shared.
+ * together changes roundings only. A softmax weight is rounded to bf16 before
+ * it multiplies its V row, as in tree_verify_attention; a row's parts are fp16
+ * times a power of two (half a step 2^-11 of them), sums fp32.
+ *
+ * Whether keys are taken together is chosen by the sizes that the host knows:
+ * where reading shared rows once can save less than joining the parts costs
+ * (few K/V bytes, or query rows of a sequence and KV head that nearly fill
+ * blocks of 256, as 64 nodes x 4 heads do), the batch runs as if nothing were
+ * shared. shared_len is not among them: every sequence is taken to share up to
+ * max_kv_len tokens. A batch that shares little beside what its sequences have
+ * of their own is up to half as long again as tree_verify_attention on it.
  *
  *   groups       number of groups, 0 <= groups <= 256; with 0 the two arrays
- *                may be NULL and every sequence is attended by itself
+ *                may be NULL and every sequence is attended by itself. Groups
+ *                may be empty, but all count: with groups >= B nothing is
+ *                shared. (With the sequences that share nothing first or last
+ *                in the batch, arrays of B / 2 groups hold any grouping.)
  *   group_start  [groups + 1] int32, ascending: group s is the sequences
  *                group_start[s] .. group_start[s + 1] - 1. Sequences before the
  *                first group or behind the last one are attended by themselves.
@@ -266,7 +276,7 @@ TV_API int kv_compact_accepted(const uint16_t *k_tree, const uint16_t *v_tree, u
  * by every row, and may be anything).
  * A start that is not ascending counts as the largest before it, one outside
  * [0, B] is clamped. Where the pages of a group's sequences differ below
- * shared_len, results are unspecified. Calls captured into graphs that may
+ * shared_len, results are unspecified (tv_validate_inputs does not look). Calls captured into graphs that may
  * run at the same time need workspaces of their own.
  * Supported: as tree_verify_attention, with 0 <= B <= 512,
  * B * N * Hq * D <= 2^34 and max_pages * P < 2^31.
@@ -347,7 +357,9 @@ TV_API int kv_accumulate_weights(const uint16_t *q, const float *lse, const uint
  *
  *   k_cache, v_cache  [num_pages, P, Hkv, D] bf16, rows moved in place; no page
  *                     id below L of a sequence may occur twice among the slots
- *                     from fixed_len on, in this or in another sequence
+ *                     from fixed_len on, in this or in another sequence (not
+ *                     checked, nor by tv_validate_inputs: rows of the other
+ *                     sequence would be overwritten)
  *   weight, position  [B, Hkv, T] fp32 / int32, T = max_pages * P
  *   weight_out, position_out  [B, Hkv, T]: each may be the array it updates;
  *                     slots below kept_len[b] are written, nothing else

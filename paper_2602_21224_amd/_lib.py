@@ -346,7 +346,8 @@ def tree_verify_attention_shared(q, k_tree, v_tree, k_cache, v_cache, page_table
                                  workspace=None, stream=None):
     """tree_verify_attention for a batch whose sequences share prefixes: sequences
     group_start[s] .. group_start[s+1]-1 hold their first shared_len[s] tokens in the
-    same pages, and those rows are read once for the whole group. group_start
+    same pages, and those rows are read once for the whole group, where that can pay
+    (not with as many groups as sequences, empty ones among them). group_start
     [groups + 1] and shared_len [groups] are int32 (both None: no groups).
     Returns (out bf16 [B,N,Hq,D], lse fp32 [B,N,Hq] or None)."""
     B, N, Hq, D = q.shape
@@ -438,6 +439,7 @@ def kv_evict(weight, position, k_cache, v_cache, page_table, kv_len, seen, *, ma
     ones, those of the `recent` newest positions, then the heaviest. The kept rows past
     that length move into the evicted slots below it (K, V, weight, position). Updates
     the caches, and `weight` and `position` unless other arrays are given for them.
+    `kept_len` may not overlap kv_len, seen or fixed_len.
     Returns (weight_out, position_out, kept_len)."""
     num_pages, P, Hkv, D = k_cache.shape
     B, max_pages = page_table.shape

@@ -22,8 +22,9 @@
 //     global_load_lds_dwordx4 (no register staging). Each 256-byte row is
 //     stored with its 16-byte chunks XOR-swizzled by the key index, so the
 //     MFMA operand reads below are free of bank conflicts. Keys past the
-//     prefix, and tree slots past N, load a harmless finite row (tree node 0)
-//     and are masked; the NaN-filled tail slots of a cache page are never read.
+//     prefix, and tree slots past N, load a row that exists, of V tree node 0's
+//     (finite), and are masked; the NaN-filled tail slots of a cache page are
+//     never read.
 //   * Each wave owns 32 query rows; the workgroup's 8 waves step through the
 //     tiles together, one workgroup barrier per 64-key tile ("period"). In
 //     period j every wave computes S^T = K_j Q^T with

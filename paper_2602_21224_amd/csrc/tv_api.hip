@@ -153,7 +153,7 @@ SharedShape shared_shape(int N, int Hq, int Hkv) {
 // 46. Row blocks of eight waves also have to save more tiles than they cost, by the count
 // that the kernel makes of each group: 29 sequences of 273 rows over 154 tokens 118 and 133.
 bool sharing_pays(const AttnShape &s, int B, int Hkv, int D, int groups, long max_len) {
-    if (groups == 0 || groups >= B) return false;            // one sequence per group
+    if (groups == 0 || groups >= B) return false;            // one sequence per group (empty ones count)
     if ((long)(B - groups) * Hkv * D * 4 * max_len < 32l << 20) return false;
     const long block = 8 * tv::kRowsPerWave, padded = (s.rows + block - 1) / block * block;
     if ((padded - s.rows) * 4 < padded) return false;
