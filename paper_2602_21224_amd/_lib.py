@@ -304,6 +304,14 @@ def _want_on(dev, t, name, dtypes, shape=None):
         raise ValueError(f"{name} is on {t.device}, expected cuda:{dev}")
 
 
+def _size(x):
+    """A bound or budget as the C entry points' int: ctypes passes the low 32 bits of any
+    integer, which made a budget of 2^40 one of 0. No sequence has 2^31 tokens, so more than
+    that is that; what is negative stays so and is refused there."""
+    x = int(x)
+    return x if 0 <= x <= 0x7FFFFFFF else -1 if x < 0 else 0x7FFFFFFF
+
+
 _current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
 
 
@@ -389,7 +397,7 @@ def tree_verify_attention_shared(q, k_tree, v_tree, k_cache, v_cache, page_table
           _ptr(q), _ptr(k_tree), _ptr(v_tree), _ptr(k_cache), _ptr(v_cache), _ptr(page_table),
           _ptr(kv_len), _ptr(parent), _ptr(num_nodes), _ptr(group_start if groups else None),
           _ptr(shared_len if groups else None), groups, B, N, Hq, Hkv, D, P, max_pages, num_pages,
-          int(max_kv_len), float(scale), _ptr(out), _ptr(lse), _ptr(workspace), workspace.numel())
+          _size(max_kv_len), float(scale), _ptr(out), _ptr(lse), _ptr(workspace), workspace.numel())
     return out, lse
 
 
@@ -424,7 +432,7 @@ def kv_accumulate_weights(q, lse, k_cache, page_table, kv_len, accept_idx, accep
     _call("kv_accumulate_weights", dev, stream, (),
           _ptr(q), _ptr(lse), _ptr(k_cache), _ptr(page_table), _ptr(kv_len), _ptr(accept_idx),
           _ptr(accept_len), _ptr(seen), _ptr(fixed_len), _ptr(weight), B, N, Hq, Hkv, D, P,
-          max_pages, num_pages, int(max_kv_len), float(scale), _ptr(weight_out), _ptr(position))
+          max_pages, num_pages, _size(max_kv_len), float(scale), _ptr(weight_out), _ptr(position))
     return weight_out, position
 
 
@@ -474,7 +482,7 @@ def kv_evict(weight, position, k_cache, v_cache, page_table, kv_len, seen, *, ma
     _call("kv_evict", dev, stream, own,
           _ptr(weight), _ptr(position), _ptr(k_cache), _ptr(v_cache), _ptr(page_table),
           _ptr(kv_len), _ptr(seen), _ptr(fixed_len), B, Hkv, D, P, max_pages, num_pages,
-          int(max_kv_len), int(budget), int(recent), _ptr(weight_out), _ptr(position_out),
+          _size(max_kv_len), _size(budget), _size(recent), _ptr(weight_out), _ptr(position_out),
           _ptr(kept_len), _ptr(workspace), workspace.numel())
     return weight_out, position_out, kept_len
 
