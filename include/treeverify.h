@@ -386,6 +386,122 @@ TV_API int kv_evict(const float *weight, const int32_t *position, uint16_t *k_ca
                     size_t workspace_bytes, hipStream_t stream);
 
 /* ------------------------------------------------------------------------
+ * tree_verify_attention_window
+ *
+ * tree_verify_attention for a layer that looks back over a sliding window and
+ * always sees a few first tokens (sinks). Node i of sequence b stands at
+ * position kv_len[b] + depth(i) (steps from its root), prefix key t at t, and a
+ * key that tree_verify_attention shows node i (the prefix, itself, its
+ * ancestors) is visible iff its position t has
+ *   t < sinks  or  t > kv_len[b] + depth(i) - window
+ * so a node sees `window` positions up to its own. window = 0 shows all (and
+ * sinks is not used). Only tiles of 64 keys with a visible key are read: the
+ * work is that of a prefix of about window + sinks tokens.
+ *
+ * Slots are positions here: a cache that kv_evict has shortened has no window.
+ * Prefix positions that no node of the sequence sees (sinks <= t <= kv_len[b] -
+ * window, the slots past kv_len[b]) may hold anything, and pages of which no
+ * position is visible may be given back: their page-table entries may be
+ * anything too (tv_validate_inputs does not know the window and asks for the
+ * whole prefix's pages). Rows that some nodes of a sequence see and others do
+ * not (V of the tree's nodes and of the window's last positions, which deeper
+ * nodes have left behind) are finite: their weight 0 does not hide an infinity
+ * or NaN.
+ *
+ * Arguments, layouts and limits are tree_verify_attention's, with
+ * max_pages * P <= 2^31 - 1025, window, sinks >= 0, and
+ * tv_window_attention_workspace_size(...) bytes of workspace. Softmax weights
+ * are rounded to bf16 before they multiply V, a split row's parts to fp16 times
+ * a power of two (half a step 2^-11), sums are fp32. Calls captured into graphs
+ * that may run at the same time need workspaces of their own.
+ * ------------------------------------------------------------------------ */
+TV_API size_t tv_window_attention_workspace_size(int B, int N, int Hq, int Hkv, int D);
+
+TV_API int tree_verify_attention_window(const uint16_t *q, const uint16_t *k_tree,
+                                        const uint16_t *v_tree, const uint16_t *k_cache,
+                                        const uint16_t *v_cache, const int32_t *page_table,
+                                        const int32_t *kv_len, const int32_t *parent,
+                                        const int32_t *num_nodes, int B, int N, int Hq, int Hkv,
+                                        int D, int P, int max_pages, int num_pages,
+                                        int max_kv_len, int window, int sinks, float scale,
+                                        uint16_t *out, float *lse, void *workspace,
+                                        size_t workspace_bytes, hipStream_t stream);
+
+/* ------------------------------------------------------------------------
+ * The cache in 4 bits
+ *
+ * kv4_write and tree_verify_attention_kv4 keep the paged cache in blocks of 32
+ * values along the head dimension that share a power of two: 4.25 bits a value,
+ * 136 bytes per key and KV head (K and V) at head size 128 where bf16 takes 512.
+ *   k4, v4   [num_pages, Hkv, P, D/2] uint8: value 2i of a row in the low four
+ *            bits of byte i, value 2i+1 in the high four. A code is a sign
+ *            (bit 3) and 0, 0.5, 1, 1.5, 2, 3, 4, 6 for 0 .. 7.
+ *   scales   [num_pages, Hkv, P, 2, D/32] uint8: of each block of the K row,
+ *            then of the V row, the exponent e of its power of two plus 127.
+ *            255: every value of the block is NaN.
+ * A value is its code's times 2^e; every one is exact in bf16 (from 2^128 on,
+ * which kv4_write does not make, it is infinite). Tokens of a page lie together
+ * per KV head: [Hkv, P], not [P, Hkv] as in the bf16 cache.
+ * ------------------------------------------------------------------------
+ * kv4_write
+ *
+ * Rows of K and V into that cache: a prompt, a chunk of one, a token, or the
+ * accepted path (with idx = accept_idx, count = accept_len, start = kv_len it is
+ * kv_compact_accepted). For j < n_b = count[b] (clamped to [0, T]; NULL: T):
+ *   source row  k[b][idx[b,j]], v[b][idx[b,j]]   (idx NULL: row j)
+ *   position    start[b] + j, through the page table
+ * and of every block of 32 values, with a its largest magnitude:
+ *   e     the smallest exponent >= -126 with a <= 7 * 2^e, at most 125
+ *   code  of the representable value nearest to v / 2^e (what exceeds 6 becomes
+ *         6), ties to the even code; the sign is kept, also of zeros
+ * A block that holds a NaN or an infinity becomes NaN whole (codes 0). No other
+ * byte of the cache is written. Rows whose source, position or page id is out of
+ * range are skipped (contract violation); no two rows may go to the same place
+ * (not checked).
+ *
+ *   k, v        [B, T, Hkv, D]  bf16
+ *   page_table  [B, max_pages]  int32; start [B] int32 (may be kv_len: read only)
+ *   idx         [B, T] int32 or NULL; count [B] int32 or NULL
+ *   k_held, v_held  [B, T, Hkv, D] bf16, or NULL: row j < n_b gets the values that
+ *               the cache now holds for it (what later tokens will see), other
+ *               rows are left as they are. k_held may be k and v_held v where idx
+ *               is NULL; any other overlap of them with k, v or each other is
+ *               refused (TV_ERR_OVERLAP).
+ * Supported: 0 <= B <= 65535; T >= 0; Hkv >= 1 with ceil(T / 16) * Hkv < 2^24;
+ * D in {64, 128}; P a power of two in [1, 256]; max_pages * P < 2^31. All arrays
+ * but the int32 ones 16-byte aligned.
+ * ------------------------------------------------------------------------ */
+TV_API int kv4_write(const uint16_t *k, const uint16_t *v, uint8_t *k4, uint8_t *v4,
+                     uint8_t *scales, const int32_t *page_table, const int32_t *start,
+                     const int32_t *idx, const int32_t *count, int B, int T, int Hkv, int D,
+                     int P, int max_pages, int num_pages, uint16_t *k_held, uint16_t *v_held,
+                     hipStream_t stream);
+
+/* ------------------------------------------------------------------------
+ * tree_verify_attention_kv4
+ *
+ * tree_verify_attention_window's function (window = 0: tree_verify_attention's)
+ * over that cache: K and V of the prefix are the values that the codes stand
+ * for, the tree's own rows are bf16. What that declaration says of positions,
+ * of rows that may hold anything and of roundings holds here; a block of NaN
+ * reaches the rows that see it, like a NaN of the bf16 cache.
+ * Arguments, layouts and limits are tree_verify_attention_window's, with k4, v4
+ * and scales (16-byte aligned) in place of k_cache and v_cache, and
+ * tv_kv4_attention_workspace_size(...) bytes of workspace.
+ * ------------------------------------------------------------------------ */
+TV_API size_t tv_kv4_attention_workspace_size(int B, int N, int Hq, int Hkv, int D);
+
+TV_API int tree_verify_attention_kv4(const uint16_t *q, const uint16_t *k_tree,
+                                     const uint16_t *v_tree, const uint8_t *k4, const uint8_t *v4,
+                                     const uint8_t *scales, const int32_t *page_table,
+                                     const int32_t *kv_len, const int32_t *parent,
+                                     const int32_t *num_nodes, int B, int N, int Hq, int Hkv,
+                                     int D, int P, int max_pages, int num_pages, int max_kv_len,
+                                     int window, int sinks, float scale, uint16_t *out,
+                                     float *lse, void *workspace, size_t workspace_bytes,
+                                     hipStream_t stream);
+
+/* ------------------------------------------------------------------------
  * tv_validate_inputs (debug aid)
  *
  * Checks the content contract on the device and writes a bit set to

@@ -9,6 +9,8 @@ __all__ = ["tree_verify_attention", "tree_argmax_accept", "tree_argmax_accept_no
            "kv_compact_accepted",
            "tree_verify_attention_shared", "kv_accumulate_weights", "kv_evict",
            "shared_attention_workspace_size", "evict_workspace_size",
+           "tree_verify_attention_window", "kv4_write", "tree_verify_attention_kv4",
+           "window_attention_workspace_size", "kv4_attention_workspace_size",
            "tv_validate_inputs", "tree_build", "tree_resample", "tree_lm_head_argmax_accept",
            "attention_workspace_size", "lm_head_workspace_size",
            "argmax_workspace_size", "tree_build_workspace_size", "abi_version", "load"]

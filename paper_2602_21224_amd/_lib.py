@@ -75,6 +75,16 @@ def load():
     lib.tv_evict_workspace_size.restype = sz
     lib.kv_evict.argtypes = [p] * 8 + [i] * 9 + [p] * 4 + [sz, p]
     lib.kv_evict.restype = i
+    lib.tv_window_attention_workspace_size.argtypes = [i] * 5
+    lib.tv_window_attention_workspace_size.restype = sz
+    lib.tree_verify_attention_window.argtypes = [p] * 9 + [i] * 11 + [ctypes.c_float, p, p, p, sz, p]
+    lib.tree_verify_attention_window.restype = i
+    lib.tv_kv4_attention_workspace_size.argtypes = [i] * 5
+    lib.tv_kv4_attention_workspace_size.restype = sz
+    lib.tree_verify_attention_kv4.argtypes = [p] * 10 + [i] * 11 + [ctypes.c_float, p, p, p, sz, p]
+    lib.tree_verify_attention_kv4.restype = i
+    lib.kv4_write.argtypes = [p] * 9 + [i] * 7 + [p] * 3
+    lib.kv4_write.restype = i
     _lib = lib
     return lib
 
@@ -485,6 +495,113 @@ def kv_evict(weight, position, k_cache, v_cache, page_table, kv_len, seen, *, ma
           _size(max_kv_len), _size(budget), _size(recent), _ptr(weight_out), _ptr(position_out),
           _ptr(kept_len), _ptr(workspace), workspace.numel())
     return weight_out, position_out, kept_len
+
+
+def window_attention_workspace_size(B, N, Hq, Hkv, D) -> int:
+    return int(load().tv_window_attention_workspace_size(B, N, Hq, Hkv, D))
+
+
+def kv4_attention_workspace_size(B, N, Hq, Hkv, D) -> int:
+    return int(load().tv_kv4_attention_workspace_size(B, N, Hq, Hkv, D))
+
+
+def _long_attention(what, size, q, k_tree, v_tree, cache, page_table, kv_len, parent, P, num_pages, max_kv_len,
+                    window, sinks, num_nodes, scale, out, lse, want_lse, workspace, stream):
+    """The two calls with a window, behind the checks of their caches."""
+    B, N, Hq, D = q.shape
+    Hkv = k_tree.shape[2]
+    max_pages = page_table.shape[1]
+    dev = q.get_device()
+    _want_on(dev, k_tree, "k_tree", _BF16, (B, N, Hkv, D))
+    _want_on(dev, v_tree, "v_tree", _BF16, (B, N, Hkv, D))
+    _want_on(dev, page_table, "page_table", _I32, (B, max_pages))
+    _want_on(dev, kv_len, "kv_len", _I32, (B,))
+    _want_on(dev, parent, "parent", _I32, (B, N))
+    if num_nodes is not None:
+        _want_on(dev, num_nodes, "num_nodes", _I32, (B,))
+    own = []
+    if out is None:
+        out = _own(dev, stream, (B, N, Hq, D), torch.bfloat16)
+        own.append(out)
+    _want_on(dev, out, "out", _BF16, (B, N, Hq, D))
+    if lse is None and want_lse:
+        lse = _own(dev, stream, (B, N, Hq), torch.float32)
+        own.append(lse)
+    if lse is not None:
+        _want_on(dev, lse, "lse", _F32, (B, N, Hq))
+    if workspace is None:
+        workspace = _own(dev, stream, max(size(B, N, Hq, Hkv, D), 16), torch.uint8)
+    _want_on(dev, workspace, "workspace", _U8)
+    _call(what, dev, stream, own, _ptr(q), _ptr(k_tree), _ptr(v_tree), *cache, _ptr(page_table), _ptr(kv_len),
+          _ptr(parent), _ptr(num_nodes), B, N, Hq, Hkv, D, P, max_pages, num_pages, _size(max_kv_len), _size(window),
+          _size(sinks), float(scale), _ptr(out), _ptr(lse), _ptr(workspace), workspace.numel())
+    return out, lse
+
+
+def tree_verify_attention_window(q, k_tree, v_tree, k_cache, v_cache, page_table, kv_len, parent, *,
+                                 max_kv_len: int, window: int, sinks: int = 0, num_nodes=None, scale: float = 0.0,
+                                 out=None, lse=None, want_lse: bool = True, workspace=None, stream=None):
+    """tree_verify_attention of a layer that looks back over `window` positions (0: all),
+    a node's own included, and always sees the first `sinks`. Pages that hold no visible
+    position may have been given back.
+    Returns (out bf16 [B,N,Hq,D], lse fp32 [B,N,Hq] or None)."""
+    _want(q, "q", _BF16)
+    num_pages, P = k_cache.shape[0], k_cache.shape[1]
+    shape = (num_pages, P, k_tree.shape[2], q.shape[3])
+    dev = q.get_device()
+    _want_on(dev, k_cache, "k_cache", _BF16, shape)
+    _want_on(dev, v_cache, "v_cache", _BF16, shape)
+    return _long_attention("tree_verify_attention_window", window_attention_workspace_size, q, k_tree, v_tree,
+                           (_ptr(k_cache), _ptr(v_cache)), page_table, kv_len, parent, P, num_pages, max_kv_len,
+                           window, sinks, num_nodes, scale, out, lse, want_lse, workspace, stream)
+
+
+def _want_cache4(dev, k4, v4, scales, Hkv, D):
+    """Checks a cache in 4 bits; returns (num_pages, P)."""
+    num_pages, P = k4.shape[0], k4.shape[2]
+    _want_on(dev, k4, "k4", _U8, (num_pages, Hkv, P, D // 2))
+    _want_on(dev, v4, "v4", _U8, (num_pages, Hkv, P, D // 2))
+    _want_on(dev, scales, "scales", _U8, (num_pages, Hkv, P, 2, D // 32))
+    return num_pages, P
+
+
+def tree_verify_attention_kv4(q, k_tree, v_tree, k4, v4, scales, page_table, kv_len, parent, *, max_kv_len: int,
+                              window: int = 0, sinks: int = 0, num_nodes=None, scale: float = 0.0, out=None,
+                              lse=None, want_lse: bool = True, workspace=None, stream=None):
+    """tree_verify_attention over a cache in 4 bits, as kv4_write fills it: k4 and v4 uint8
+    [num_pages, Hkv, P, D/2], scales uint8 [num_pages, Hkv, P, 2, D/32]. `window` and
+    `sinks` as for tree_verify_attention_window.
+    Returns (out bf16 [B,N,Hq,D], lse fp32 [B,N,Hq] or None)."""
+    _want(q, "q", _BF16)
+    num_pages, P = _want_cache4(q.get_device(), k4, v4, scales, k_tree.shape[2], q.shape[3])
+    return _long_attention("tree_verify_attention_kv4", kv4_attention_workspace_size, q, k_tree, v_tree,
+                           (_ptr(k4), _ptr(v4), _ptr(scales)), page_table, kv_len, parent, P, num_pages, max_kv_len,
+                           window, sinks, num_nodes, scale, out, lse, want_lse, workspace, stream)
+
+
+def kv4_write(k, v, k4, v4, scales, page_table, start, *, idx=None, count=None, k_held=None, v_held=None, stream=None):
+    """Write rows [B, T, Hkv, D] bf16 of K and V into a cache in 4 bits at positions
+    start[b] + j, j < count[b] (int32 [B]; None: T), from row idx[b, j] (int32 [B, T];
+    None: j). With `k_held`, `v_held` (bf16 [B, T, Hkv, D]) the values that the cache
+    then holds go there. Returns (k4, v4, scales)."""
+    B, T, Hkv, D = k.shape
+    dev = k.get_device()
+    _want(k, "k", _BF16)
+    _want_on(dev, v, "v", _BF16, (B, T, Hkv, D))
+    num_pages, P = _want_cache4(dev, k4, v4, scales, Hkv, D)
+    max_pages = page_table.shape[1]
+    _want_on(dev, page_table, "page_table", _I32, (B, max_pages))
+    _want_on(dev, start, "start", _I32, (B,))
+    if idx is not None:
+        _want_on(dev, idx, "idx", _I32, (B, T))
+    if count is not None:
+        _want_on(dev, count, "count", _I32, (B,))
+    for t, name in ((k_held, "k_held"), (v_held, "v_held")):
+        if t is not None:
+            _want_on(dev, t, name, _BF16, (B, T, Hkv, D))
+    _call("kv4_write", dev, stream, (), _ptr(k), _ptr(v), _ptr(k4), _ptr(v4), _ptr(scales), _ptr(page_table),
+          _ptr(start), _ptr(idx), _ptr(count), B, T, Hkv, D, P, max_pages, num_pages, _ptr(k_held), _ptr(v_held))
+    return k4, v4, scales
 
 
 def tv_validate_inputs(page_table, kv_len, parent, *, P: int, num_pages: int, num_nodes=None,

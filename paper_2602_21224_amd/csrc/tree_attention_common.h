@@ -127,6 +127,58 @@ __device__ __forceinline__ int tiles_of_sequence(int L, int nodes, const AttnPar
     return p.Hkv * tiles_per_head((L + KT - 1) / KT, nodes * p.G, p);
 }
 
+// What the window leaves of a prefix of L tokens for a sequence's nodes together: positions
+// [lo, L), which its roots see (a node d steps below its root sees from lo0 + d on), and
+// [0, sinks). In 64-key tiles: the first ns and those from ns + gap on.
+struct Span {
+    int lo0, lo, sinks, ns, gap;
+};
+__device__ __forceinline__ Span span_of(int L, const WindowAttnParams &p) {
+    Span s;
+    s.lo0 = p.window > 0 ? L - p.window + 1 : -kMaxNodes;
+    s.lo = max(s.lo0, 0);
+    s.sinks = p.sinks;
+    s.ns = min((min(s.sinks, s.lo) + KT - 1) / KT, s.lo / KT);
+    s.gap = s.lo / KT - s.ns;
+    return s;
+}
+__device__ __forceinline__ Span span_of(int, const AttnParams &) { return Span{-kMaxNodes, 0, 0, 0, 0}; }
+__device__ __forceinline__ int tiles_of_sequence(int L, int nodes, const WindowAttnParams &p) {
+    return p.Hkv * tiles_per_head((L + KT - 1) / KT - span_of(L, p).gap, nodes * p.G, p);
+}
+
+// Keys of the prefix tile at position `base` that a node d steps below its root sees.
+__device__ __forceinline__ unsigned long long window_bits(const Span &sp, int base, int d) {
+    const int from = min(max(sp.lo0 + d - base, 0), KT), to = min(max(sp.sinks - base, 0), KT);
+    return (from < KT ? ~0ull << from : 0ull) | (to < KT ? (1ull << to) - 1ull : ~0ull);
+}
+// Whether every node of a sequence of at most N sees all of that tile.
+__device__ __forceinline__ bool window_clear(const Span &sp, int base, int N) {
+    return base >= sp.lo0 + N - 1 || base + KT <= sp.sinks;
+}
+// Steps from node i to its root (the ancestor sets are reflexive).
+__device__ __forceinline__ int depth_of(const unsigned long long (&anc)[4]) {
+    return __popcll(anc[0]) + __popcll(anc[1]) + __popcll(anc[2]) + __popcll(anc[3]) - 1;
+}
+// Word w of a node's root path as far as the window shows it: an ancestor's place among the
+// path's nodes is its depth, and its position L + depth.
+__device__ __forceinline__ unsigned long long window_path(const unsigned long long (&anc)[4], int w, int L,
+                                                          const WindowAttnParams &p) {
+    unsigned long long x = anc[w];
+    const int first = max(p.sinks - L, 0), last = depth_of(anc) - p.window;      // depths not seen
+    if (p.window <= 0 || last < first) return x;
+    int d = 0;
+    for (int u = 0; u < w; ++u) d += __popcll(anc[u]);
+    unsigned long long seen = 0;
+    for (; x; x &= x - 1, ++d)
+        if (d < first || d > last) seen |= x & -x;
+    return seen;
+}
+__device__ __forceinline__ unsigned long long window_path(const unsigned long long (&anc)[4], int w, int,
+                                                          const AttnParams &) {
+    return anc[w];
+}
+
 // Explicit LDS wait for reads issued through inline assembly; `tie` makes a
 // fragment's later uses depend on the wait (volatile asm keeps its order).
 template <int N>
@@ -183,8 +235,8 @@ __device__ __forceinline__ float part_scale(float top, float &unscale) {
 // clamped prefix lengths into g_len[0..B) and the node counts into g_nn:
 // wave 0 reads kv_len (and num_nodes) once per lane and scans with cross-lane
 // shifts, one barrier for the whole workgroup.
-template <int NT>
-__device__ void build_cumulative(const AttnParams &p) {
+template <int NT, typename Params>
+__device__ void build_cumulative(const Params &p) {
     if (threadIdx.x < kWave) {
         const int lane = threadIdx.x;
         int carry = 0;
@@ -321,7 +373,9 @@ __device__ void build_ancestor_masks_wave_lds(const AttnParams &p, int b) {
     }
 }
 
-template <int D, int NW, bool SMALL>
+// WIN: some positions below L are not to be read into a product: those behind the window,
+// from sink_end to lo - 1. Their pages may have been given back.
+template <int D, int NW, bool SMALL, bool WIN = false>
 struct TileIssue {
     using Gm = Geo<D>;
     static constexpr int kLoadsPerWave = Gm::kBlocksPerTile / NW;   // per K (or V) tile
@@ -336,6 +390,7 @@ struct TileIssue {
         const char *k[LPT];
         const char *v[LPT];
         int nv[LPT];
+        int pos[WIN ? LPT : 1];                       // WIN: position of the block's first key
     };
 
     int kib;                                          // this lane's key within a block
@@ -347,6 +402,9 @@ struct TileIssue {
     const char *kt_g, *vt_g;                          // tree row of node 0, KV head g
     unsigned row_bytes, page_bytes;                   // key row of all KV heads; one page
     int L, ntp, nodes;
+    int lo, sink_end;                                 // WIN
+
+    __device__ __forceinline__ bool live(int pos) const { return !WIN || pos >= lo || pos < sink_end; }
 
     __device__ __forceinline__ void init(int wave_u, int lane, const AttnParams &p) {
         row_bytes = (unsigned)(p.Hkv * D * 2);
@@ -371,6 +429,7 @@ struct TileIssue {
         const int pos_w = t * KT + wave_u * LPT * KPB;
         if (LPT * KPB > p.P || t >= ntp || t * KT + KT > L || (unsigned)pg0 >= (unsigned)p.num_pages)
             return false;
+        if (WIN && t * KT < lo && t * KT + KT > sink_end) return false;
         off = (unsigned long long)(unsigned)pg0 * page_bytes + (unsigned)(pos_w & (p.P - 1)) * row_bytes;
         return true;
     }
@@ -434,6 +493,7 @@ struct TileIssue {
                 r.k[i] = ok ? kc_g + off : kt_g;
                 r.v[i] = ok ? vc_g + off : vt_g;
                 r.nv[i] = !ok ? 0 : (full ? KPB : min(L - pos0, KPB));
+                if (WIN) r.pos[i] = pos0;
             }
         } else {
             #pragma unroll
@@ -444,6 +504,7 @@ struct TileIssue {
                 r.k[i] = kt_g + off;
                 r.v[i] = vt_g + off;
                 r.nv[i] = nv;
+                if (WIN) r.pos[i] = lo;               // tree rows are seen or masked, not left out
             }
         }
         return r;
@@ -460,7 +521,7 @@ struct TileIssue {
         unsigned char *dst = g_ring + stage * Gm::kStageBytes + (is_v ? Gm::kTileBytes : 0);
         #pragma unroll
         for (int i = 0; i < LPT; ++i) {
-            const bool in = kib < bl.nv[i];
+            const bool in = kib < bl.nv[i] && (!WIN || live(bl.pos[i] + kib));
             const char *addr = (is_v ? bl.v[i] : bl.k[i]) + ((in ? row_off : 0u) + chunk_off[i]);
             LDS_AS void *to = (LDS_AS void *)(dst + (wave_u * LPT + i) * 1024);
             if (SMALL || !is_v || in)
@@ -474,12 +535,16 @@ struct TileIssue {
     // LDS page-id window (prefix tiles only).
     __device__ __forceinline__ void issue_small(const AttnParams &p, int t, bool is_v, int page_first,
                                                 int wave_u) const {
-        unsigned char *dst = g_ring + (t & (NS - 1)) * Gm::kStageBytes + (is_v ? Gm::kTileBytes : 0);
+        issue_small(p, t, is_v, page_first, wave_u, t & (NS - 1));
+    }
+    __device__ __forceinline__ void issue_small(const AttnParams &p, int t, bool is_v, int page_first, int wave_u,
+                                                int stage) const {
+        unsigned char *dst = g_ring + stage * Gm::kStageBytes + (is_v ? Gm::kTileBytes : 0);
         #pragma unroll
         for (int i = 0; i < LPT; ++i) {
             const int pos = t * KT + (wave_u * LPT + i) * KPB + kib;
             const char *row = is_v ? vt_g : kt_g;
-            if (pos < L) {
+            if (pos < L && live(pos)) {
                 const int id = g_pages[(pos >> p.p_shift) - page_first];
                 if (id >= 0)
                     row = (is_v ? vc_g : kc_g) + (size_t)(unsigned)id * page_bytes + (size_t)(pos & (p.P - 1)) * row_bytes;

@@ -1,0 +1,47 @@
+// Tree-masked attention inside a sliding window over a bf16 cache, for gfx950: the kernels
+// of tree_attention.hip with a unit's prefix tiles cut to those that hold a visible key.
+//
+// Node i stands at position L + depth(i) and sees, of the prefix and of its root path, the
+// positions t > L + depth(i) - window and t < sinks. The prefix tiles are the sinks' and
+// those from the root's first visible position on, so the work is that of a prefix of about
+// window + sinks tokens whatever L; only tiles at an edge are masked, per row, by the row's
+// depth. Keys that no node sees are not read into a product, so their pages may be given
+// back and their slots hold anything. Pieces of split units are kept in fp16 times a power
+// of two per row, as in tree_verify_attention_shared.
+#include "tree_attention_kernel.h"
+
+namespace tv {
+namespace {
+
+template <int D, int NW, bool NARROW>
+hipError_t launch_main(const WindowAttnParams &p, hipStream_t s) {
+    auto go = [&](auto kernel) { return launch_kernel(kernel, dim3(p.num_wg), dim3(NW * kWave), s, p); };
+    if (p.whole_units)
+        return p.small_pages ? go(tree_attention_kernel<D, NW, true, NARROW, true, false, true>)
+                             : go(tree_attention_kernel<D, NW, false, NARROW, true, false, true>);
+    return p.small_pages ? go(tree_attention_kernel<D, NW, true, NARROW, false, true, true>)
+                         : go(tree_attention_kernel<D, NW, false, NARROW, false, true, true>);
+}
+
+template <int D>
+hipError_t launch_d(const WindowAttnParams &p, int waves, hipStream_t s) {
+    const hipError_t e = waves == 8  ? launch_main<D, 8, false>(p, s)
+                         : p.narrow ? launch_main<D, 4, true>(p, s)
+                                    : launch_main<D, 4, false>(p, s);
+    if (e != hipSuccess || p.num_wg == 1 || p.whole_units) return e;
+    constexpr int kRowsPerWg = 256 / (D / 8);
+    const int chunks = (p.rows_per_block + kRowsPerWg - 1) / kRowsPerWg;
+    const int stride = (p.num_wg + kNumXcd - 1) / kNumXcd * kNumXcd;
+    return launch_kernel(tree_attention_merge_fine_kernel<D>, dim3(stride * chunks), dim3(256), s,
+                         static_cast<const AttnParams &>(p), stride);
+}
+
+}  // namespace
+
+hipError_t launch_window_attention(const WindowAttnParams &p, int head_dim, int waves, hipStream_t s) {
+    if (head_dim == 64) return launch_d<64>(p, waves, s);
+    if (head_dim == 128) return launch_d<128>(p, waves, s);
+    return hipErrorInvalidValue;
+}
+
+}  // namespace tv

@@ -241,6 +241,27 @@ long shared_places(const SharedShape &s, int B, int N, int Hkv, int D, int group
     return Hkv * (shared_blocks(s, B, groups) * prefix + B * own);
 }
 
+// Whether each unit is taken whole by a workgroup of its own, over `tiles` prefix tiles at most.
+// Short units are not worth splitting: one workgroup per unit saves the merge
+// launch and the partials it reads, 3-4 us, for about 1.2 us per tile of a
+// unit of at most 16 rows or of head size 64, and 2 us of the others. While the
+// units leave CUs idle, long ones (several row blocks, or one-token pages of head
+// size 128, each load a page) are split a tile sooner. Measured (us per call,
+// whole and split): 16 rows of 64, 4 tiles 10.5 and 12.6; 16 rows of 128, 4 tiles
+// 13.0 and 13.9, with one-token pages 64 units 14.4 and 13.8, 128 units 13.0 and
+// 14.4; 132 rows of 128, 3 tiles 14.5 and 16.4; 256 rows of 128, 3 tiles 14.9 and
+// 15.0, 4 tiles 16.9 and 15.0; 512 rows of 64, 4 tiles, 16 units 15.9 and 15.4;
+// 1024 rows of 64, 4 tiles, 8 units 14.4 and 13.7; 2048 rows of 64, 4 tiles, 16
+// units 18.8 and 17.3; 2048 rows of 128, 3 tiles, 16 units 20.0 and 18.8.
+bool whole_units(const AttnShape &s, int B, int N, int Hkv, int D, long tiles, bool small_pages, int max_wg) {
+    const long units = (long)B * Hkv * s.row_blocks;
+    const long unit_tiles = tiles + (N + tv::kKeyTile - 1) / tv::kKeyTile;
+    const bool sooner = D == 64          ? s.rows > 256 && units < 128
+                        : s.rows <= 16 ? small_pages && units < 128
+                                       : s.rows > 512 && units < 32;
+    return units <= max_wg && unit_tiles <= (D == 64 || s.rows <= 16 ? 4 : 3) - (sooner ? 1 : 0);
+}
+
 // tree_verify_attention behind its argument checks; `fine`: see launch_tree_attention.
 int launch_attention(bool fine, const uint16_t *q, const uint16_t *k_tree, const uint16_t *v_tree,
                      const uint16_t *k_cache, const uint16_t *v_cache, const int32_t *page_table, const int32_t *kv_len,
@@ -259,25 +280,10 @@ int launch_attention(bool fine, const uint16_t *q, const uint16_t *k_tree, const
     long num_wg = attn_tiles(s, B, Hkv, hint_len) / kMinShareTiles;
     if (num_wg < 1) num_wg = 1;
     if (num_wg > max_wg) num_wg = max_wg;
-    // Short units are not worth splitting: one workgroup per unit saves the merge
-    // launch and the partials it reads, 3-4 us, for about 1.2 us per tile of a
-    // unit of at most 16 rows or of head size 64, and 2 us of the others. While the
-    // units leave CUs idle, long ones (several row blocks, or one-token pages of head
-    // size 128, each load a page) are split a tile sooner. Measured (us per call,
-    // whole and split): 16 rows of 64, 4 tiles 10.5 and 12.6; 16 rows of 128, 4 tiles
-    // 13.0 and 13.9, with one-token pages 64 units 14.4 and 13.8, 128 units 13.0 and
-    // 14.4; 132 rows of 128, 3 tiles 14.5 and 16.4; 256 rows of 128, 3 tiles 14.9 and
-    // 15.0, 4 tiles 16.9 and 15.0; 512 rows of 64, 4 tiles, 16 units 15.9 and 15.4;
-    // 1024 rows of 64, 4 tiles, 8 units 14.4 and 13.7; 2048 rows of 64, 4 tiles, 16
-    // units 18.8 and 17.3; 2048 rows of 128, 3 tiles, 16 units 20.0 and 18.8.
-    const long units = (long)B * Hkv * s.row_blocks;
-    const long unit_tiles = (hint_len + tv::kKeyTile - 1) / tv::kKeyTile + (N + tv::kKeyTile - 1) / tv::kKeyTile;
     const bool small_pages = P < 1024 / (2 * D);
-    const bool sooner = D == 64          ? s.rows > 256 && units < 128
-                        : s.rows <= 16 ? small_pages && units < 128
-                                       : s.rows > 512 && units < 32;
-    const bool whole = units <= max_wg && unit_tiles <= (D == 64 || s.rows <= 16 ? 4 : 3) - (sooner ? 1 : 0);
-    if (whole) num_wg = units;
+    const bool whole =
+        whole_units(s, B, N, Hkv, D, (hint_len + tv::kKeyTile - 1) / tv::kKeyTile, small_pages, max_wg);
+    if (whole) num_wg = (long)B * Hkv * s.row_blocks;
 
     tv::AttnParams p;
     p.q = q; p.k_tree = k_tree; p.v_tree = v_tree; p.k_cache = k_cache; p.v_cache = v_cache;
@@ -303,6 +309,54 @@ int launch_attention(bool fine, const uint16_t *q, const uint16_t *k_tree, const
     return tv::launch_tree_attention(p, D, s.waves, fine, stream) == hipSuccess ? TV_OK : TV_ERR_HIP;
 }
 
+// What the calls with a window have in common: limits of sizes, prefix tiles of a unit, and
+// the parameters that do not depend on the kernel.
+bool window_shape_ok(int B, int N, int Hq, int Hkv, int D, int P, int max_pages, int num_pages, int max_kv_len,
+                     int window, int sinks) {
+    return attn_shape_ok(B, N, Hq, Hkv, D) && pow2(P) && P <= 256 && max_pages >= 1 && num_pages >= 1 &&
+           max_kv_len >= 0 && window >= 0 && sinks >= 0 &&
+           // positions, those of the nodes too, are ints
+           (long)max_pages * P <= 0x7FFFFFFFl - 4 * tv::kMaxNodes;
+}
+
+long window_tiles(long len, int window, int sinks) {
+    const long all = (len + tv::kKeyTile - 1) / tv::kKeyTile;
+    if (window == 0) return all;
+    const long some = ((long)window + tv::kKeyTile - 2) / tv::kKeyTile + 1 + ((long)sinks + tv::kKeyTile - 1) / tv::kKeyTile;
+    return all < some ? all : some;
+}
+
+void window_params(tv::WindowAttnParams &p, const uint16_t *q, const uint16_t *k_tree, const uint16_t *v_tree,
+                   const int32_t *page_table, const int32_t *kv_len, const int32_t *parent, const int32_t *num_nodes,
+                   int B, int N, int Hq, int Hkv, int D, int P, int max_pages, int num_pages, int window, int sinks,
+                   float scale, uint16_t *out, float *lse, void *workspace, const AttnWorkspace &ws) {
+    p.q = q; p.k_tree = k_tree; p.v_tree = v_tree;
+    p.page_table = page_table; p.kv_len = kv_len; p.parent = parent; p.num_nodes = num_nodes;
+    p.out = out; p.lse = lse;
+    char *base = static_cast<char *>(workspace);
+    p.ws_o = reinterpret_cast<uint16_t *>(base);
+    p.ws_ml = reinterpret_cast<float *>(base + ws.o_bytes);
+    p.ws_desc = reinterpret_cast<int32_t *>(base + ws.o_bytes + ws.ml_bytes);
+    p.B = B; p.N = N; p.Hq = Hq; p.Hkv = Hkv; p.G = Hq / Hkv;
+    p.P = P; p.p_shift = __builtin_ctz((unsigned)P);
+    p.max_pages = max_pages; p.num_pages = num_pages;
+    p.scale = scale > 0.f ? scale : 1.0f / sqrtf((float)D);
+    p.scale_log2 = p.scale * 1.4426950408889634f;
+    p.window = window; p.sinks = sinks;
+}
+
+// Attention over a cache in 4 bits: one to four 16-row tiles per wave, rows beyond 64 in
+// blocks of 64.
+constexpr int kKv4SetupTiles = 4;
+constexpr int kKv4MinShareTiles = 8;
+
+AttnShape kv4_shape(int N, int Hq, int Hkv) {
+    AttnShape s = attn_shape(N, Hq, Hkv);
+    s.rows_per_block = s.rows <= 16 ? 16 : s.rows <= 32 ? 32 : 64;
+    s.row_blocks = (s.rows + s.rows_per_block - 1) / s.rows_per_block;
+    s.tree_tiles_all = s.row_blocks * ((N + tv::kKeyTile - 1) / tv::kKeyTile);      // at most
+    return s;
+}
 
 }  // namespace
 
@@ -609,6 +663,126 @@ int kv_evict(const float *weight, const int32_t *position, uint16_t *k_cache, ui
     const long cap = (long)max_pages * P;
     p.max_keys = (int)(max_kv_len < cap ? max_kv_len : cap);
     return tv::launch_evict(p, stream) == hipSuccess ? TV_OK : TV_ERR_HIP;
+}
+
+size_t tv_window_attention_workspace_size(int B, int N, int Hq, int Hkv, int D) {
+    if (!attn_shape_ok(B, N, Hq, Hkv, D)) return 0;
+    return attn_workspace(attn_shape(N, Hq, Hkv), D, cu_count() * kWgPerCu, true).total;
+}
+
+int tree_verify_attention_window(const uint16_t *q, const uint16_t *k_tree, const uint16_t *v_tree,
+                                 const uint16_t *k_cache, const uint16_t *v_cache, const int32_t *page_table,
+                                 const int32_t *kv_len, const int32_t *parent, const int32_t *num_nodes, int B, int N,
+                                 int Hq, int Hkv, int D, int P, int max_pages, int num_pages, int max_kv_len,
+                                 int window, int sinks, float scale, uint16_t *out, float *lse, void *workspace,
+                                 size_t workspace_bytes, hipStream_t stream) {
+    if (!window_shape_ok(B, N, Hq, Hkv, D, P, max_pages, num_pages, max_kv_len, window, sinks)) return TV_ERR_SHAPE;
+    if (B == 0) return TV_OK;
+    if (!q || !k_tree || !v_tree || !k_cache || !v_cache || !page_table || !kv_len || !parent || !out || !workspace)
+        return TV_ERR_NULL;
+    if (!aligned16(q) || !aligned16(k_tree) || !aligned16(v_tree) || !aligned16(k_cache) || !aligned16(v_cache) ||
+        !aligned16(out) || !aligned16(workspace))
+        return TV_ERR_ALIGN;
+    const AttnShape s = attn_shape(N, Hq, Hkv);
+    const int max_wg = cu_count() * kWgPerCu;
+    const AttnWorkspace ws = attn_workspace(s, D, max_wg, true);
+    if (workspace_bytes < ws.total) return TV_ERR_WORKSPACE;
+    const long max_len = (long)max_pages * P;
+    if (attn_tiles(s, B, Hkv, max_len) >= kMaxTiles) return TV_ERR_SHAPE;
+    if (!device_ok()) return TV_ERR_DEVICE;
+
+    tv::WindowAttnParams p{};
+    window_params(p, q, k_tree, v_tree, page_table, kv_len, parent, num_nodes, B, N, Hq, Hkv, D, P, max_pages, num_pages,
+                  window, sinks, scale, out, lse, workspace, ws);
+    p.k_cache = k_cache; p.v_cache = v_cache;
+    // the launch of tree_verify_attention over as many tiles as the window leaves
+    const long tiles = window_tiles(max_kv_len < max_len ? max_kv_len : max_len, window, sinks);
+    long num_wg = attn_tiles(s, B, Hkv, tiles * tv::kKeyTile) / kMinShareTiles;
+    if (num_wg < 1) num_wg = 1;
+    if (num_wg > max_wg) num_wg = max_wg;
+    const bool small_pages = P < 1024 / (2 * D);
+    const bool whole = whole_units(s, B, N, Hkv, D, tiles, small_pages, max_wg);
+    if (whole) num_wg = (long)B * Hkv * s.row_blocks;
+    p.rows_per_block = s.rows_per_block;
+    p.setup_tiles = kSetupTiles;
+    p.small_pages = small_pages ? 1 : 0;
+    p.narrow = s.rows <= 16 ? 1 : 0;
+    p.num_wg = (int)num_wg;
+    p.whole_units = whole ? 1 : 0;
+    return tv::launch_window_attention(p, D, s.waves, stream) == hipSuccess ? TV_OK : TV_ERR_HIP;
+}
+
+size_t tv_kv4_attention_workspace_size(int B, int N, int Hq, int Hkv, int D) {
+    if (!attn_shape_ok(B, N, Hq, Hkv, D)) return 0;
+    return attn_workspace(kv4_shape(N, Hq, Hkv), D, cu_count() * kWgPerCu, true).total;
+}
+
+int tree_verify_attention_kv4(const uint16_t *q, const uint16_t *k_tree, const uint16_t *v_tree, const uint8_t *k4,
+                              const uint8_t *v4, const uint8_t *scales, const int32_t *page_table,
+                              const int32_t *kv_len, const int32_t *parent, const int32_t *num_nodes, int B, int N,
+                              int Hq, int Hkv, int D, int P, int max_pages, int num_pages, int max_kv_len, int window,
+                              int sinks, float scale, uint16_t *out, float *lse, void *workspace,
+                              size_t workspace_bytes, hipStream_t stream) {
+    if (!window_shape_ok(B, N, Hq, Hkv, D, P, max_pages, num_pages, max_kv_len, window, sinks)) return TV_ERR_SHAPE;
+    if (B == 0) return TV_OK;
+    if (!q || !k_tree || !v_tree || !k4 || !v4 || !scales || !page_table || !kv_len || !parent || !out || !workspace)
+        return TV_ERR_NULL;
+    if (!aligned16(q) || !aligned16(k_tree) || !aligned16(v_tree) || !aligned16(k4) || !aligned16(v4) ||
+        !aligned16(scales) || !aligned16(out) || !aligned16(workspace))
+        return TV_ERR_ALIGN;
+    const AttnShape s = kv4_shape(N, Hq, Hkv);
+    const int max_wg = cu_count() * kWgPerCu;
+    const AttnWorkspace ws = attn_workspace(s, D, max_wg, true);
+    if (workspace_bytes < ws.total) return TV_ERR_WORKSPACE;
+    auto tiles_of = [&](long tiles) {
+        return (long)B * Hkv * ((long)s.row_blocks * (tiles + kKv4SetupTiles) + s.tree_tiles_all);
+    };
+    const long max_len = (long)max_pages * P;
+    if (tiles_of((max_len + tv::kKeyTile - 1) / tv::kKeyTile) >= kMaxTiles) return TV_ERR_SHAPE;
+    if (!device_ok()) return TV_ERR_DEVICE;
+
+    tv::Kv4AttnParams p{};
+    window_params(p, q, k_tree, v_tree, page_table, kv_len, parent, num_nodes, B, N, Hq, Hkv, D, P, max_pages, num_pages,
+                  window, sinks, scale, out, lse, workspace, ws);
+    p.k4 = k4; p.v4 = v4; p.scales = scales;
+    long num_wg = tiles_of(window_tiles(max_kv_len < max_len ? max_kv_len : max_len, window, sinks)) / kKv4MinShareTiles;
+    if (num_wg < 1) num_wg = 1;
+    if (num_wg > max_wg) num_wg = max_wg;
+    p.rows_per_block = s.rows_per_block;
+    p.setup_tiles = kKv4SetupTiles;
+    p.num_wg = (int)num_wg;
+    return tv::launch_kv4_attention(p, D, stream) == hipSuccess ? TV_OK : TV_ERR_HIP;
+}
+
+int kv4_write(const uint16_t *k, const uint16_t *v, uint8_t *k4, uint8_t *v4, uint8_t *scales,
+              const int32_t *page_table, const int32_t *start, const int32_t *idx, const int32_t *count, int B, int T,
+              int Hkv, int D, int P, int max_pages, int num_pages, uint16_t *k_held, uint16_t *v_held,
+              hipStream_t stream) {
+    if (B < 0 || B > 65535 || T < 0 || Hkv < 1 || (D != 64 && D != 128) || !pow2(P) || P > 256 || max_pages < 1 ||
+        num_pages < 1 || (long)max_pages * P >= (1l << 31))
+        return TV_ERR_SHAPE;
+    // workgroups of 256 threads per sequence: fewer than 2^32 threads
+    if (((long)T + 15) / 16 * Hkv >= (1l << 24)) return TV_ERR_SHAPE;
+    if (B == 0 || T == 0) return TV_OK;
+    if (!k || !v || !k4 || !v4 || !scales || !page_table || !start) return TV_ERR_NULL;
+    if (!aligned16(k) || !aligned16(v) || !aligned16(k4) || !aligned16(v4) || !aligned16(scales) ||
+        !aligned16(k_held) || !aligned16(v_held))
+        return TV_ERR_ALIGN;
+    // held rows may take their own rows' place, which the thread that writes has read; no others'
+    const size_t bytes = (size_t)B * T * Hkv * D * sizeof(uint16_t);
+    auto meet = [&](const uint16_t *x, const uint16_t *y) {
+        const uintptr_t a = reinterpret_cast<uintptr_t>(x), b = reinterpret_cast<uintptr_t>(y);
+        return x && y && (a < b ? b - a : a - b) < bytes;
+    };
+    if (meet(k_held, v) || meet(v_held, k) || meet(k_held, v_held) || (meet(k_held, k) && (idx || k_held != k)) ||
+        (meet(v_held, v) && (idx || v_held != v)))
+        return TV_ERR_OVERLAP;
+    if (!device_ok()) return TV_ERR_DEVICE;
+    tv::Kv4WriteParams p;
+    p.k = k; p.v = v; p.k4 = k4; p.v4 = v4; p.scales = scales; p.page_table = page_table; p.start = start;
+    p.idx = idx; p.count = count; p.k_held = k_held; p.v_held = v_held;
+    p.T = T; p.Hkv = Hkv; p.p_shift = __builtin_ctz((unsigned)P); p.max_pages = max_pages; p.num_pages = num_pages;
+    return tv::launch_kv4_write(p, B, D, stream) == hipSuccess ? TV_OK : TV_ERR_HIP;
 }
 
 int tv_validate_inputs(const int32_t *page_table, const int32_t *kv_len, const int32_t *parent,

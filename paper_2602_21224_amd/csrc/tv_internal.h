@@ -87,6 +87,18 @@ struct AttnParams {
     int whole_units;             // every workgroup takes one unit whole (nothing to merge)
 };
 
+// The same inside a sliding window.
+struct WindowAttnParams : AttnParams {
+    int window;                  // positions that a node looks back over, itself included; 0: all
+    int sinks;                   // first positions that every node sees
+};
+
+// The same over a cache held in 4 bits (k_cache and v_cache are null).
+struct Kv4AttnParams : WindowAttnParams {
+    const uint8_t *k4, *v4;      // [num_pages][Hkv][P][D / 2] codes
+    const uint8_t *scales;       // [num_pages][Hkv][P][2][D / 32]: K's, V's
+};
+
 // The same for batches with shared prefixes.
 struct SharedAttnParams : AttnParams {
     const int32_t *group_start, *shared_len;
@@ -135,6 +147,16 @@ struct EvictParams {
     int vector_out;              // and stored
     int chunk_shift;             // log2 of a row's 16-byte pieces, or -1
     int move_here;               // the selecting workgroup moves the rows itself
+};
+
+// Launch parameters of the write into a cache held in 4 bits (all sizes in elements).
+struct Kv4WriteParams {
+    const uint16_t *k, *v;
+    uint8_t *k4, *v4, *scales;
+    const int32_t *page_table, *start;
+    const int32_t *idx, *count;  // [B, T] or null (row j is j), [B] or null (T)
+    uint16_t *k_held, *v_held;   // or null
+    int T, Hkv, p_shift, max_pages, num_pages;
 };
 
 // Inclusive sums and (of numbers >= 0) maxima over the lanes of a wave, without LDS:
@@ -226,6 +248,9 @@ hipError_t launch_kv_compact(const uint16_t *k_tree, const uint16_t *v_tree, uin
 hipError_t launch_shared_attention(const SharedAttnParams &p, int head_dim, hipStream_t s);
 hipError_t launch_accumulate_weights(const WeightParams &p, int head_dim, hipStream_t s);
 hipError_t launch_evict(EvictParams p, hipStream_t s);
+hipError_t launch_window_attention(const WindowAttnParams &p, int head_dim, int waves, hipStream_t s);
+hipError_t launch_kv4_attention(const Kv4AttnParams &p, int head_dim, hipStream_t s);
+hipError_t launch_kv4_write(const Kv4WriteParams &p, int B, int head_dim, hipStream_t s);
 hipError_t launch_validate(const int32_t *page_table, const int32_t *kv_len,
                            const int32_t *parent, const int32_t *num_nodes, int B, int N, int P,
                            int max_pages, int num_pages, int32_t *status_word, hipStream_t s);

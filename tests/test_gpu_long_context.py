@@ -1,0 +1,442 @@
+"""GPU parity of the long-context operators against the CPU oracle: the write into a cache
+of 4 bits, tree attention over it, tree attention inside a window, and a run of them."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import long_context as O
+from paper_2602_21224_amd import workloads as W
+from tests import gpu_util as U
+from tests import long_util as LU
+
+pytestmark = pytest.mark.gpu
+
+CASES = [
+    # B, N, Hq, Hkv, D, P, lens, window, sinks, tree, ragged
+    (1, 1, 8, 8, 64, 16, [128], 0, 0, "chain", False),            # the smallest
+    (1, 1, 1, 1, 128, 16, [0], 0, 0, "chain", False),             # no prefix, one node: v itself
+    (3, 1, 8, 2, 128, 16, [0, 1, 63], 0, 0, "chain", False),      # decoding, short prefixes
+    (4, 1, 32, 8, 128, 16, [700, 64, 65, 1029], 0, 0, "chain", False),
+    (40, 1, 16, 4, 64, 2, (0, 300), 0, 0, "chain", True),         # a larger batch, sequences without nodes
+    (3, 12, 8, 8, 128, 16, [300, 0, 129], 0, 0, "capped", False), # 12 rows
+    (2, 9, 4, 2, 64, 1, [77, 500], 0, 0, "forest", False),        # 18 rows, one-token pages
+    (3, 24, 2, 2, 128, 8, [200, 64, 3], 0, 0, "forest", True),    # 24 rows
+    (2, 45, 24, 8, 64, 1, [301, 777], 0, 0, "forest", True),      # 135 rows, odd
+    (2, 64, 8, 2, 128, 16, [130, 1000], 0, 0, "capped", False),   # 256 rows
+    (2, 100, 12, 2, 128, 64, [640, 0], 0, 0, "chain", True),      # 600 rows
+    (1, 256, 8, 1, 64, 256, [700], 0, 0, "capped", False),        # 2048 rows, long pages
+    (1, 256, 2, 1, 128, 32, [190], 0, 0, "chain", False),         # the deepest tree
+    # inside a window
+    (1, 1, 8, 8, 64, 16, [128], 1, 0, "chain", False),            # a token sees itself
+    (3, 1, 8, 2, 128, 16, [700, 64, 5], 1, 3, "chain", False),
+    (4, 1, 32, 8, 128, 16, [2000, 99, 100, 101], 100, 4, "chain", False),
+    (4, 1, 8, 2, 64, 1, [700, 64, 65, 1029], 64, 64, "chain", False),     # edges on tile borders
+    (3, 1, 8, 2, 128, 4, [640, 127, 128], 129, 130, "chain", False),      # sinks over two tiles
+    (2, 12, 8, 8, 128, 16, [900, 40], 77, 5, "chain", False),
+    (2, 12, 8, 8, 128, 16, [900, 40], 5, 0, "chain", False),      # a window shorter than the tree
+    (3, 9, 4, 2, 64, 2, [77, 500, 3], 3, 80, "chain", False),     # sinks that reach into the tree
+    (3, 16, 4, 4, 128, 16, [257, 0, 300], 1, 2, "forest", True),  # the window is one token: roots and sinks
+    (5, 45, 24, 8, 64, 1, [301, 777, 0, 201, 202], 201, 5, "forest", True),
+    (2, 64, 8, 2, 128, 16, [1300, 1000], 500, 17, "capped", False),
+    (2, 64, 8, 2, 128, 16, [1300, 60], 30, 0, "chain", False),    # deep chain, short window
+    (2, 100, 12, 2, 128, 64, [640, 1999], 333, 1, "chain", True),
+    (1, 200, 4, 2, 64, 256, [1500], 90, 300, "chain", False),     # far edges within the tree, several words
+    (1, 256, 8, 1, 128, 16, [700], 650, 9, "capped", False),
+    (2, 3, 16, 2, 128, 1, [5000, 2500], 1200, 70, "chain", False),    # one-token pages, several page windows
+    (1, 1, 2, 1, 64, 1, [20000], 0, 0, "chain", False),           # one unit over all workgroups
+    (1, 1, 2, 1, 128, 1, [20000], 9000, 700, "chain", False),
+]
+
+
+def attend(T, w, window, sinks, cache=None, d=None, **kw):
+    d = d or U.upload(w)
+    args = (d["page_table"], d["kv_len"], d["parent"])
+    kw = dict(max_kv_len=w.max_kv_len, window=window, sinks=sinks, num_nodes=d["num_nodes"], **kw)
+    if cache is None:
+        return T.tree_verify_attention_window(d["q"], d["k_tree"], d["v_tree"], d["k_cache"], d["v_cache"], *args, **kw)
+    return T.tree_verify_attention_kv4(d["q"], d["k_tree"], d["v_tree"], *[U.dev(a) for a in cache], *args, **kw)
+
+
+def check(w, out, lse, want, label):
+    LU.check(w, U.bf16_to_f64(out), lse.cpu().numpy().astype(np.float64), want, label)
+
+
+def same(a, b):
+    return torch.equal(a.view(torch.int16), b.view(torch.int16))
+
+
+def case_workload(case):
+    B, N, Hq, Hkv, D, P, lens, window, sinks, tree, ragged = CASES[case]
+    w = LU.workload(900 + case, B=B, N=N, Hq=Hq, Hkv=Hkv, D=D, P=P, lens=lens, window=window, sinks=sinks, tree=tree,
+                    ragged=ragged)
+    print(f"case {case}: {CASES[case]} lens={w.kv_len.tolist()} nodes={w.num_nodes}", flush=True)
+    return w, window, sinks
+
+
+@pytest.mark.parametrize("case", range(len(CASES)))
+def test_window(case):
+    T = U.require_gpu()
+    w, window, sinks = case_workload(case)
+    out, lse = attend(T, w, window, sinks)
+    check(w, out, lse, LU.expected(w, window, sinks), f"window {case}")
+    again, lse2 = attend(T, w, window, sinks)
+    assert same(out, again) and torch.equal(lse, lse2)
+
+
+@pytest.mark.parametrize("case", range(len(CASES)))
+def test_kv4(case):
+    T = U.require_gpu()
+    w, window, sinks = case_workload(case)
+    cache = LU.cache4(w)
+    out, lse = attend(T, w, window, sinks, cache)
+    check(w, out, lse, LU.expected(w, window, sinks, cache), f"kv4 {case}")
+    again, lse2 = attend(T, w, window, sinks, cache)
+    assert same(out, again) and torch.equal(lse, lse2)
+
+
+@pytest.mark.parametrize("case", [3, 8, 9, 10])
+def test_without_a_window_the_plain_attention(case):
+    T = U.require_gpu()
+    w, _, _ = case_workload(case)
+    d = U.upload(w)
+    out, lse = attend(T, w, 0, 77, d=d)
+    want, z = T.tree_verify_attention(d["q"], d["k_tree"], d["v_tree"], d["k_cache"], d["v_cache"], d["page_table"],
+                                      d["kv_len"], d["parent"], max_kv_len=w.max_kv_len, num_nodes=d["num_nodes"])
+    real = torch.isfinite(z)
+    assert torch.equal(real, torch.isfinite(lse)) and (lse[real] - z[real]).abs().max() < 1e-4
+    assert (out.float() - want.float()).abs().max() < 2e-2
+    wide, lse2 = attend(T, w, 0x7FFFFFFF, 0x7FFFFFFF, d=d)
+    assert same(out, wide) and torch.equal(lse, lse2)
+
+
+@pytest.mark.parametrize("cached", ["bf16", "4 bits"])
+@pytest.mark.parametrize("hint", [0, 1, 100, 1 << 20, 1 << 40])
+def test_the_bound_of_the_lengths_changes_no_result_beyond_rounding(cached, hint):
+    T = U.require_gpu()
+    w = LU.workload(31, B=3, N=5, Hq=8, Hkv=2, D=128, P=16, lens=[900, 0, 333], window=250, sinks=20, tree="chain")
+    cache = LU.cache4(w) if cached == "4 bits" else None
+    d = U.upload(w)
+    kw = dict(max_kv_len=hint, window=250, sinks=20)
+    if cache is None:
+        out, lse = T.tree_verify_attention_window(d["q"], d["k_tree"], d["v_tree"], d["k_cache"], d["v_cache"],
+                                                  d["page_table"], d["kv_len"], d["parent"], **kw)
+    else:
+        out, lse = T.tree_verify_attention_kv4(d["q"], d["k_tree"], d["v_tree"], *[U.dev(a) for a in cache],
+                                               d["page_table"], d["kv_len"], d["parent"], **kw)
+    check(w, out, lse, LU.expected(w, 250, 20, cache), f"{cached} {hint}")
+
+
+@pytest.mark.parametrize("cached", ["bf16", "4 bits"])
+@pytest.mark.parametrize("scale", [0.003, 0.5, 3.0])
+def test_scales(cached, scale):
+    """Nearly uniform weights, and ones that leave a single key."""
+    T = U.require_gpu()
+    w = LU.workload(32, B=2, N=6, Hq=8, Hkv=2, D=64, P=8, lens=[300, 70], tree="chain")
+    cache = LU.cache4(w) if cached == "4 bits" else None
+    out, lse = attend(T, w, 0, 0, cache, scale=scale)
+    check(w, out, lse, LU.expected(w, 0, 0, cache, scale=scale), f"{cached} scale {scale}")
+
+
+def test_without_lse_and_into_given_buffers():
+    T = U.require_gpu()
+    w, window, sinks = case_workload(22)
+    cache = LU.cache4(w)
+    d = U.upload(w)
+    for c, size in ((None, T.window_attention_workspace_size), (cache, T.kv4_attention_workspace_size)):
+        a, lse = attend(T, w, window, sinks, c, d=d)
+        out = torch.full_like(a, 7.0)
+        ws = torch.full((size(w.B, w.N, w.Hq, w.Hkv, w.D),), 255, dtype=torch.uint8, device="cuda")
+        z = torch.full_like(lse, 7.0)
+        got, none = attend(T, w, window, sinks, c, d=d, out=out, want_lse=False, workspace=ws)
+        assert none is None and got is out and same(a, out)
+        got, z2 = attend(T, w, window, sinks, c, d=d, lse=z, workspace=ws)
+        assert z2 is z and torch.equal(z, lse) and same(a, got)
+
+
+def test_a_block_of_nan_reaches_the_rows_that_see_it():
+    """One sequence has it in its prefix, the other behind its window."""
+    T = U.require_gpu()
+    w = LU.workload(34, B=2, N=1, Hq=8, Hkv=2, D=128, P=16, lens=[300, 300], window=100, sinks=2, tree="chain")
+    k4, v4, sc = LU.cache4(w)
+    clean, _ = attend(T, w, 100, 2, (k4, v4, sc))
+    page = w.page_table[0, 250 // 16]
+    sc[page, 1, 250 % 16, 1, 2] = 255            # V of KV head 1, columns 64 .. 95
+    out, lse = attend(T, w, 100, 2, (k4, v4, sc))
+    nan = torch.isnan(out)
+    assert nan[0, :, 4:, 64:96].all() and nan.sum() == 4 * 32 and torch.isfinite(lse).all()
+    assert same(clean[~nan], out[~nan])
+    sc[page, 1, 250 % 16, 1, 2] = 127
+    sc[page, 0, 250 % 16, 0, 0] = 255            # K of KV head 0
+    out, lse = attend(T, w, 100, 2, (k4, v4, sc))
+    assert torch.isnan(lse[0, :, :4]).all() and torch.isfinite(lse[0, :, 4:]).all() and torch.isfinite(lse[1]).all()
+
+
+def test_every_scale_byte_and_code():
+    """Keys of one block per scale byte; a single key is visible, so out is its values."""
+    T = U.require_gpu()
+    N = 255
+    w = LU.workload(35, B=N, N=1, Hq=1, Hkv=1, D=64, P=1, lens=[1] * N, tree="chain")
+    k4, v4, sc = LU.cache4(w)
+    w.q[:] = 0
+    k4[:] = 0
+    w.v_tree[:] = 0
+    for b in range(N):
+        page = w.page_table[b, 0]
+        v4[page, 0, 0] = [(2 * i % 16) + 16 * ((2 * i + 1) % 16) for i in range(32)]
+        sc[page] = 127
+        sc[page, 0, 0, 1] = b
+    out, _ = attend(T, w, 0, 0, (k4, v4, sc))
+    want = 0.5 * O.dequantize4(v4, sc[..., 1, :])[w.page_table[:, 0], 0, 0]
+    got = U.bf16_to_f64(out)[:, 0, 0]
+    fits = (np.abs(want) < 2.0 ** 126) & ((np.abs(want) >= 2.0 ** -125) | (want == 0))
+    assert fits[5:250].all() and np.array_equal(got[fits], want[fits])
+
+
+# ---------------------------------------------------------------------------
+# the write
+# ---------------------------------------------------------------------------
+
+WRITES = [
+    # B, T, Hkv, D, P, starts, idx, count
+    (1, 1, 8, 64, 16, [128], False, False),
+    (1, 1, 1, 128, 1, [0], False, False),
+    (3, 7, 2, 128, 16, [0, 15, 100], False, True),
+    (2, 64, 8, 128, 16, [33, 1000], True, True),
+    (5, 77, 5, 64, 1, [0, 3, 300, 299, 1], False, True),
+    (2, 300, 3, 128, 256, [0, 200], False, False),
+    (1, 33, 4, 64, 2, [5], True, False),
+    (40, 3, 2, 64, 8, list(range(40)), True, True),
+]
+
+
+def write_inputs(case, seed=50):
+    B, T, Hkv, D, P, start, with_idx, with_count = WRITES[case]
+    rng = np.random.default_rng(seed + case)
+    x = rng.standard_normal((2, B, T, Hkv, D)) * np.exp2(rng.integers(-3, 4, size=(2, B, T, Hkv, D // 32)).repeat(32, -1))
+    k, v = W.f32_to_bf16_bits(x[0].astype(np.float32)), W.f32_to_bf16_bits(x[1].astype(np.float32))
+    start = np.asarray(start, np.int32)
+    table, pages = W.paged_layout(rng, start, T, P)
+    idx = rng.integers(0, T, size=(B, T)).astype(np.int32) if with_idx else None     # the same row twice too
+    count = rng.integers(0, T + 1, size=B).astype(np.int32) if with_count else None
+    fill = lambda *s: rng.integers(0, 256, size=s).astype(np.uint8)  # noqa: E731
+    return dict(k=k, v=v, k4=fill(pages, Hkv, P, D // 2), v4=fill(pages, Hkv, P, D // 2),
+                scales=fill(pages, Hkv, P, 2, D // 32), page_table=table, start=start, idx=idx, count=count)
+
+
+def write(T, s, held=True, **kw):
+    up = lambda a: None if a is None else U.dev(a)  # noqa: E731
+    k, v = U.dev_bf16(s["k"]), U.dev_bf16(s["v"])
+    kh, vh = (torch.full_like(k, 9.0), torch.full_like(k, 9.0)) if held else (None, None)
+    out = T.kv4_write(k, v, up(s["k4"]), up(s["v4"]), up(s["scales"]), up(s["page_table"]), up(s["start"]),
+                      idx=up(s["idx"]), count=up(s["count"]), k_held=kh, v_held=vh, **kw)
+    torch.cuda.synchronize()
+    return [t.cpu().numpy() for t in out], kh, vh
+
+
+@pytest.mark.parametrize("case", range(len(WRITES)))
+def test_write(case):
+    """Bit for bit, and not a byte beside what is written."""
+    T = U.require_gpu()
+    print(f"write {case}: {WRITES[case]}", flush=True)
+    s = write_inputs(case)
+    got, kh, vh = write(T, s)
+    want = O.write4(**s)
+    for a, b, name in zip(got, want, ("k4", "v4", "scales")):
+        assert np.array_equal(a, b), name
+    n = np.full(len(s["k"]), s["k"].shape[1]) if s["count"] is None else s["count"]
+    done = np.arange(s["k"].shape[1])[None, :] < n[:, None]
+    for t, b in ((kh, want[3]), (vh, want[4])):
+        t = U.bf16_to_f64(t)
+        assert np.array_equal(t[done], b[done]) and (t[~done] == 9).all()
+    plain, _, _ = write(T, s, held=False)
+    assert all(np.array_equal(a, b) for a, b in zip(got, plain))
+
+
+def test_write_of_special_values():
+    """Zeros of both signs, subnormals, the largest values, every tie, NaN and infinities."""
+    T = U.require_gpu()
+    rng = np.random.default_rng(8)
+    rows = rng.integers(0, 1 << 16, size=(1, 256, 2, 64)).astype(np.uint16)          # any bit pattern
+    rows[0, :64] = (rows[0, :64] & 0x807F) | (rng.integers(0, 255, size=(64, 2, 2, 1)).repeat(32, -1).reshape(64, 2, 64)
+                                              .astype(np.uint16) << 7)               # finite: one exponent per block
+    ties = W.f32_to_bf16_bits(np.array([4, 0.25, 0.75, 1.25, 1.75, 2.5, 3.5, 5, 6, 7, -0.25, -0.75, -1.25, -5, 0, -0.0],
+                                       np.float32))
+    rows[0, 64:72] = 0
+    rows[0, 72:80] = 0x8000
+    rows[0, 80, 0, :16] = rows[0, 80, 0, 32:48] = ties
+    rows[0, 80, 0, 16:32] = rows[0, 80, 0, 48:] = 0
+    rows[0, 81, :, :] = 0x0001                   # the smallest subnormal
+    rows[0, 82, :, :] = 0x7F7F                   # the largest
+    s = dict(k=rows, v=np.ascontiguousarray(rows[:, ::-1]), page_table=np.arange(16, dtype=np.int32)[None],
+             start=np.zeros(1, np.int32), idx=None, count=None, k4=np.zeros((16, 2, 16, 32), np.uint8),
+             v4=np.zeros((16, 2, 16, 32), np.uint8), scales=np.zeros((16, 2, 16, 2, 2), np.uint8))
+    got, kh, vh = write(T, s)
+    want = O.write4(**s)
+    for a, b, name in zip(got, want, ("k4", "v4", "scales")):
+        assert np.array_equal(a, b), name
+    assert np.array_equal(U.bf16_to_f64(kh), want[3], equal_nan=True)
+    assert np.array_equal(U.bf16_to_f64(vh), want[4], equal_nan=True)
+
+
+def test_write_skips_rows_out_of_range_and_counts_outside():
+    T = U.require_gpu()
+    s = write_inputs(2)
+    s["count"] = np.array([99, -3, 7], np.int32)             # clamped: 7, 0, 7
+    s["idx"] = np.tile(np.arange(7, dtype=np.int32), (3, 1))
+    s["idx"][0, 2], s["idx"][0, 3] = -1, 7
+    table = s["page_table"].copy()
+    s["page_table"][2, 100 // 16] = len(s["k4"])             # rows 100 .. 106 of sequence 2 have no page
+    got, kh, _ = write(T, s)
+    s2 = dict(s, count=np.array([7, 0, 0]), page_table=table, idx=np.clip(s["idx"], 0, 6))
+    k4, v4, sc, hk, _ = O.write4(**s2)
+    page = table[0, 0]
+    for j in (2, 3):                                         # the two skipped rows as they were
+        for a, b in ((k4, s["k4"]), (v4, s["v4"]), (sc, s["scales"])):
+            a[page, :, j] = b[page, :, j]
+    assert np.array_equal(got[0], k4) and np.array_equal(got[1], v4) and np.array_equal(got[2], sc)
+    held = U.bf16_to_f64(kh)
+    assert (held[0, 2:4] == 9).all() and (held[1:] == 9).all() and np.array_equal(held[0, 4:], hk[0, 4:])
+    s = write_inputs(0)
+    s["start"] = np.array([-1], np.int32)
+    assert np.array_equal(write(T, s)[0][0], s["k4"])
+    s["start"] = np.array([s["page_table"].shape[1] * 16], np.int32)
+    assert np.array_equal(write(T, s)[0][0], s["k4"])
+
+
+def test_held_rows_may_replace_their_own():
+    T = U.require_gpu()
+    s = write_inputs(5)
+    want = O.write4(**s)
+    k, v = U.dev_bf16(s["k"]), U.dev_bf16(s["v"])
+    got = T.kv4_write(k, v, U.dev(s["k4"]), U.dev(s["v4"]), U.dev(s["scales"]), U.dev(s["page_table"]), U.dev(s["start"]),
+                      k_held=k, v_held=v)
+    assert np.array_equal(got[2].cpu().numpy(), want[2]) and np.array_equal(got[0].cpu().numpy(), want[0])
+    assert np.array_equal(U.bf16_to_f64(k), want[3]) and np.array_equal(U.bf16_to_f64(v), want[4])
+
+
+def test_nothing_to_write():
+    T = U.require_gpu()
+    s = write_inputs(0)
+    for shape in ((0, 1, 8, 64), (1, 0, 8, 64)):
+        k = torch.zeros(shape, dtype=torch.bfloat16, device="cuda")
+        got = T.kv4_write(k, k, U.dev(s["k4"]), U.dev(s["v4"]), U.dev(s["scales"]), U.dev(s["page_table"][:shape[0]]),
+                          U.dev(s["start"][:shape[0]]))
+        assert np.array_equal(got[0].cpu().numpy(), s["k4"])
+
+
+# ---------------------------------------------------------------------------
+# together
+# ---------------------------------------------------------------------------
+
+@pytest.mark.parametrize("window,sinks", [(0, 0), (90, 3)])
+def test_a_serving_loop_over_four_bits(oracle_mod, window, sinks):
+    """Prompts in, then several steps: verify, accept, write the accepted path, advance; the
+    pages behind the window are given back as it moves on. Every step's attention against
+    the oracle over the bytes that are in the cache."""
+    T = U.require_gpu()
+    rng = np.random.default_rng(77)
+    B, N, Hq, Hkv, D, P, steps = 3, 13, 8, 2, 128, 16, 4
+    lens = np.array([150, 0, 37], np.int32)
+    room = steps * N
+    table, pages = W.paged_layout(rng, lens, room, P)
+    bits = lambda *s: W.f32_to_bf16_bits(rng.standard_normal(s, dtype=np.float32))  # noqa: E731
+    cache = [np.zeros((pages, Hkv, P, D // 2), np.uint8), np.zeros((pages, Hkv, P, D // 2), np.uint8),
+             np.zeros((pages, Hkv, P, 2, D // 32), np.uint8)]
+    dc = [U.dev(a) for a in cache]
+    prompt_k, prompt_v = bits(B, 150, Hkv, D), bits(B, 150, Hkv, D)
+    zero = np.zeros(B, np.int32)
+    T.kv4_write(U.dev_bf16(prompt_k), U.dev_bf16(prompt_v), *dc, U.dev(table), U.dev(zero), count=U.dev(lens))
+    cache = list(O.write4(prompt_k, prompt_v, *cache, table, zero, count=lens)[:3])
+    for step in range(steps):
+        parent = np.stack([W.tree_uniform_forest(rng, N) for _ in range(B)])
+        draft = rng.integers(0, 3, size=(B, N)).astype(np.int32)
+        logits = rng.standard_normal((B, N, 3)).astype(np.float32)
+        w = W.Workload("loop", B, N, Hq, Hkv, D, P, 3, bits(B, N, Hq, D), bits(B, N, Hkv, D), bits(B, N, Hkv, D),
+                       np.zeros((pages, P, 1, 1), np.uint16), np.zeros((pages, P, 1, 1), np.uint16), table, lens.copy(),
+                       parent, draft, logits)
+        assert all(np.array_equal(a.cpu().numpy(), b) for a, b in zip(dc, cache)), step
+        d = dict(q=U.dev_bf16(w.q), k_tree=U.dev_bf16(w.k_tree), v_tree=U.dev_bf16(w.v_tree), page_table=U.dev(table),
+                 kv_len=U.dev(lens), parent=U.dev(parent))
+        out, lse = T.tree_verify_attention_kv4(d["q"], d["k_tree"], d["v_tree"], *dc, d["page_table"], d["kv_len"],
+                                               d["parent"], max_kv_len=int(lens.max()), window=window, sinks=sinks)
+        # norms of the cached rows: at most those of the values written, and an eighth more
+        w.k_cache = prompt_k
+        check(w, out, lse, LU.expected(w, window, sinks, cache), f"step {step}")
+        _, alen, aidx, _ = T.tree_argmax_accept(U.dev(logits), U.dev(draft), d["parent"])
+        T.kv4_write(d["k_tree"], d["v_tree"], *dc, d["page_table"], d["kv_len"], idx=aidx, count=alen)
+        alen, aidx = alen.cpu().numpy(), aidx.cpu().numpy()
+        cache = list(O.write4(w.k_tree, w.v_tree, *cache, table, lens, idx=aidx, count=alen)[:3])
+        lens = lens + alen.astype(np.int32)
+        if window:
+            for b in range(B):                   # positions that no later node sees
+                for page in range(-(-sinks // P), max(int(lens[b]) - window + 1, 0) // P):
+                    if table[b, page] >= 0:
+                        cache[2][table[b, page]] = 255
+                        dc[2][int(table[b, page])] = 255
+                        table[b, page] = -1
+
+
+@pytest.mark.parametrize("window", [0, 120])
+def test_one_captured_graph(window):
+    """Write, attention over 4 bits and attention inside a window in one graph; every replay
+    on new inputs gives the eager results, with eager work between."""
+    T = U.require_gpu()
+    w = LU.workload(60, B=3, N=17, Hq=8, Hkv=2, D=128, P=16, lens=[500, 64, 3], tree="forest")
+    d = U.upload(w)
+    dc = [U.dev(a) for a in LU.cache4(w)]
+    size = (w.B, w.N, w.Hq, w.Hkv, w.D)
+    ws = [torch.empty(f(*size), dtype=torch.uint8, device="cuda") for f in (T.kv4_attention_workspace_size,
+                                                                          T.window_attention_workspace_size)]
+    idx = torch.arange(w.N, dtype=torch.int32, device="cuda").repeat(w.B, 1)
+    alen = torch.tensor([4, 1, 9], dtype=torch.int32, device="cuda")
+
+    def step(out):
+        T.kv4_write(d["k_tree"], d["v_tree"], *dc, d["page_table"], d["kv_len"], idx=idx, count=alen)
+        args = (d["page_table"], d["kv_len"], d["parent"])
+        kw = dict(max_kv_len=600, window=window, sinks=4 if window else 0)
+        T.tree_verify_attention_kv4(d["q"], d["k_tree"], d["v_tree"], *dc, *args, out=out[0], lse=out[1], workspace=ws[0],
+                                    **kw)
+        T.tree_verify_attention_window(d["q"], d["k_tree"], d["v_tree"], d["k_cache"], d["v_cache"], *args, out=out[2],
+                                       lse=out[3], workspace=ws[1], **kw)
+    new = lambda: [torch.empty_like(d["q"]), torch.empty(size[:3], device="cuda"), torch.empty_like(d["q"]),  # noqa: E731
+                   torch.empty(size[:3], device="cuda")]
+    a, b = new(), new()
+    step(a)
+    torch.cuda.synchronize()
+    stream = torch.cuda.Stream()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.stream(stream):
+        with torch.cuda.graph(graph, stream=stream):
+            step(b)
+    for k in range(4):
+        d["q"].copy_(torch.randn(d["q"].shape, device="cuda"))
+        d["k_tree"].copy_(torch.randn(d["k_tree"].shape, device="cuda"))
+        d["kv_len"].copy_(torch.tensor([500 - 100 * k, 64, 3 + 7 * k], dtype=torch.int32))
+        before = [t.clone() for t in dc]
+        graph.replay()
+        torch.cuda.synchronize()
+        after = [t.clone() for t in dc]
+        for t, x in zip(dc, before):
+            t.copy_(x)
+        step(a)
+        torch.cuda.synchronize()
+        assert all(torch.equal(x, y) for x, y in zip(after, dc)), k
+        # bit for bit: the third sequence grows into slots of its bf16 cache that hold NaN
+        assert same(a[0], b[0]) and same(a[2], b[2]) and same(a[1], b[1]) and same(a[3], b[3]), k
+
+
+def test_another_stream():
+    T = U.require_gpu()
+    w, window, sinks = case_workload(23)
+    cache = LU.cache4(w)
+    s = write_inputs(3)
+    wrote, kh, _ = write(T, s)
+    want = [attend(T, w, window, sinks), attend(T, w, window, sinks, cache)]
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    for c, (a, z) in zip((None, cache), want):
+        out, lse = attend(T, w, window, sinks, c, stream=side)
+        side.synchronize()
+        assert same(a, out) and torch.equal(z, lse)
+    got, kh2, _ = write(T, s, stream=side)
+    assert all(np.array_equal(x, y) for x, y in zip(wrote, got)) and same(kh, kh2)
