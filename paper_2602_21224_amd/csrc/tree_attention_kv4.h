@@ -1,0 +1,129 @@
+// What the two kernels of the attention over 4 bits share: how a workgroup finds its pieces
+// of work, and the loads of codes.
+#pragma once
+
+#include "kv4.h"
+#include "tree_attention_kernel.h"
+
+namespace tv {
+namespace {
+
+// Equal contiguous shares of all units' virtual tiles (a unit's set-up tiles, prefix tiles
+// and tree tiles, laid end to end), as in tree_attention.hip: workgroup u takes
+// [start_of(u), start_of(u + 1)).
+struct Shares {
+    int total, nw;
+    __device__ __forceinline__ Shares(int total_, int num_wg) : total(total_), nw(min(num_wg, total_)) {}
+    __device__ __forceinline__ int start_of(int u) const {
+        return (int)(((long long)min(u, nw) * total) / max(nw, 1));
+    }
+    __device__ __forceinline__ int owner_of(int t) const { return (int)(((long long)(t + 1) * nw - 1) / total); }
+};
+
+// The part of a unit that a share covers: real tiles t0 .. t_end - 1 of its ulen, of which
+// the first ntp are the prefix's.
+struct Piece {
+    int b, g, rb, L, nodes, rows_b, ntp, t0, t_end, ulen, slot;
+    bool complete;
+    Span sp;
+    // Place of prefix tile t among all tiles of the prefix, or of tree tile t behind them.
+    __device__ __forceinline__ int real(int t) const { return t >= sp.ns ? t + sp.gap : t; }
+};
+
+// The piece at virtual tile `pos` of the share [start, end) of workgroup w; moves pos past
+// it. False if only set-up tiles of a unit are left there. The first call of a share writes
+// the joining kernel's entry for the workgroup: the split unit whose last piece is its first.
+__device__ __forceinline__ bool next_piece(const Kv4AttnParams &p, const Shares &sh, int w, int start, int end, int &pos,
+                                           Piece &pc) {
+    int lo = 0, hi = p.B - 1;
+    while (lo < hi) {
+        const int mid = (lo + hi + 1) >> 1;
+        if (g_cum[mid] <= pos) lo = mid; else hi = mid - 1;
+    }
+    pc.b = lo;
+    pc.L = g_len[lo];
+    pc.nodes = g_nn[lo];
+    pc.rows_b = pc.nodes * p.G;
+    pc.sp = span_of(pc.L, p);
+    pc.ntp = (pc.L + KT - 1) / KT - pc.sp.gap;
+    const int C = p.setup_tiles;
+    const int per_g = tiles_per_head(pc.ntp, pc.rows_b, p);
+    int off = pos - g_cum[lo];
+    pc.g = off / per_g;
+    off -= pc.g * per_g;
+    pc.rb = 0;
+    pc.ulen = pc.ntp + tree_tiles_of_block(0, pc.rows_b, p);
+    while (off >= C + pc.ulen) {
+        off -= C + pc.ulen;
+        ++pc.rb;
+        pc.ulen = pc.ntp + tree_tiles_of_block(pc.rb, pc.rows_b, p);
+    }
+    const int v_end = min(C + pc.ulen, off + (end - pos));
+    const int unit_start = pos - off + C;              // share coordinate of the unit's real tile 0
+    if (pos == start && threadIdx.x == 0) {
+        const int wf = sh.owner_of(unit_start);
+        const bool mine = unit_start < start && sh.owner_of(unit_start + pc.ulen - 1) == w;
+        *reinterpret_cast<i32x4 *>(p.ws_desc + w * 4) =
+            mine ? i32x4{pc.b, pc.g, pc.rb | (pc.nodes << 8), wf * 2 + (unit_start <= sh.start_of(wf) ? 0 : 1)}
+                 : i32x4{-1, 0, 0, 0};
+    }
+    pos += v_end - off;
+    pc.t0 = max(off - C, 0);
+    pc.t_end = v_end - C;
+    pc.complete = pc.t0 == 0 && pc.t_end == pc.ulen;
+    pc.slot = w * 2 + (unit_start <= start ? 0 : 1);
+    return pc.t_end > pc.t0;
+}
+
+// Whether the piece has a tile whose mask depends on the nodes' root paths.
+__device__ __forceinline__ bool needs_paths(const Kv4AttnParams &p, const Piece &pc) {
+    return pc.t_end > pc.ntp ||
+           (pc.t_end > pc.sp.ns && pc.real(max(pc.t0, pc.sp.ns)) * KT < pc.sp.lo0 + p.N - 1);
+}
+
+// Row of the cache (of one KV head's tokens) that holds position pos on page id, or -1 if no
+// node sees it: past the prefix, behind the window, or on a page that does not exist.
+__device__ __forceinline__ long long row_of(const Kv4AttnParams &p, int head, int pos, int id, int L, const Span &sp) {
+    const bool live = pos < L && (pos >= sp.lo || pos < sp.sinks) && (unsigned)id < (unsigned)p.num_pages;
+    const long long row =
+        (((long long)(unsigned)id * (unsigned)p.Hkv + (unsigned)head) << p.p_shift) + (unsigned)(pos & (p.P - 1));
+    return live ? row : -1;
+}
+
+template <int N>
+__device__ __forceinline__ void load_dwords(unsigned (&to)[N], const uint8_t *from) {
+    static_assert(N == 2 || N == 4, "8 or 16 bytes");
+    if constexpr (N == 4) {
+        const u32x4 x = *reinterpret_cast<const u32x4 *>(from);
+        to[0] = x[0]; to[1] = x[1]; to[2] = x[2]; to[3] = x[3];
+    } else {
+        const u32x2 x = *reinterpret_cast<const u32x2 *>(from);
+        to[0] = x[0]; to[1] = x[1];
+    }
+}
+
+// Keys that a row of node `node` sees of the prefix tile at position `base`.
+__device__ __forceinline__ unsigned long long prefix_bits(const Kv4AttnParams &p, const Piece &pc, int base, int node) {
+    const int lim = pc.L - base;
+    unsigned long long x = lim >= KT ? ~0ull : (1ull << lim) - 1ull;
+    if (!window_clear(pc.sp, base, p.N)) x &= window_bits(pc.sp, base, depth_of(g_anc[node]));
+    return x;
+}
+
+// Rows of padding nodes (not part of any unit): zeros with lse -inf, a few nodes per workgroup.
+template <int D, int NT>
+__device__ void clear_padding(const Kv4AttnParams &p, int w) {
+    if (!p.num_nodes) return;
+    const int chunks = p.Hq * D / 8;
+    for (int idx = w; idx < p.B * p.N; idx += p.num_wg) {
+        const int b = idx / p.N, i = idx - b * p.N;
+        if (i < g_nn[b]) continue;
+        u16x8 *op = reinterpret_cast<u16x8 *>(p.out + ((size_t)b * p.N + i) * p.Hq * D);
+        for (int c = threadIdx.x; c < chunks; c += NT) op[c] = u16x8{0, 0, 0, 0, 0, 0, 0, 0};
+        if (p.lse)
+            for (int h = threadIdx.x; h < p.Hq; h += NT) p.lse[((size_t)b * p.N + i) * p.Hq + h] = kNegInf;
+    }
+}
+
+}  // namespace
+}  // namespace tv

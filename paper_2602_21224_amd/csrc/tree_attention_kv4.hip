@@ -21,8 +21,7 @@
 //     own in LDS (16-byte chunks swizzled by the key), and ds_read_b64_tr_b16 reads it
 //     transposed, with the key order that the scores' accumulators have.
 // The codes of a wave's next tile are on their way in registers while it computes one.
-#include "kv4.h"
-#include "tree_attention_kernel.h"
+#include "tree_attention_kv4.h"
 
 namespace tv {
 namespace {
@@ -45,18 +44,6 @@ struct StreamState {
     float m_run[NR], l_run[NR];
 };
 
-template <int N>
-__device__ __forceinline__ void load_dwords(unsigned (&to)[N], const uint8_t *from) {
-    static_assert(N == 2 || N == 4, "8 or 16 bytes");
-    if constexpr (N == 4) {
-        const u32x4 x = *reinterpret_cast<const u32x4 *>(from);
-        to[0] = x[0]; to[1] = x[1]; to[2] = x[2]; to[3] = x[3];
-    } else {
-        const u32x2 x = *reinterpret_cast<const u32x2 *>(from);
-        to[0] = x[0]; to[1] = x[1];
-    }
-}
-
 // Page ids of the lane's keys of the prefix tile at position `base`.
 __device__ __forceinline__ void load_ids(const Kv4AttnParams &p, int b, int base, int c, int (&ids)[4]) {
     const int32_t *row = p.page_table + (size_t)b * p.max_pages;
@@ -64,21 +51,17 @@ __device__ __forceinline__ void load_ids(const Kv4AttnParams &p, int b, int base
     for (int kb = 0; kb < 4; ++kb) ids[kb] = row[min((base + 16 * kb + c) >> p.p_shift, p.max_pages - 1)];
 }
 
-// Their codes and scales. A key that no node sees (past the prefix, behind the window,
-// on a page that does not exist) reads the cache's first row and counts as zeros.
+// Their codes and scales. A key that no node sees reads the cache's first row, and counts
+// as zeros.
 template <int D>
-__device__ __forceinline__ void load_raw(const Kv4AttnParams &p, int head, int base, int L, const Span &sp, int lane,
-                                         const int (&ids)[4], Raw4<D> &r) {
+__device__ __forceinline__ void load_raw(const Kv4AttnParams &p, const Piece &pc, int base, int lane, const int (&ids)[4],
+                                         Raw4<D> &r) {
     const int c = lane & 15, g = lane >> 4;
     r.live = 0;
     #pragma unroll
     for (int kb = 0; kb < 4; ++kb) {
-        const int pos = base + 16 * kb + c;
-        const bool live = pos < L && (pos >= sp.lo || pos < sp.sinks) && (unsigned)ids[kb] < (unsigned)p.num_pages;
-        const size_t row = live ? (((size_t)(unsigned)ids[kb] * (unsigned)p.Hkv + (unsigned)head) << p.p_shift) +
-                                      (unsigned)(pos & (p.P - 1))
-                                : 0;
-        r.live |= (unsigned)live << kb;
+        const long long at = row_of(p, pc.g, base + 16 * kb + c, ids[kb], pc.L, pc.sp), row = max(at, 0ll);
+        r.live |= (unsigned)(at >= 0) << kb;
         load_dwords(r.k[kb], p.k4 + row * (D / 2) + g * (D / 8));
         load_dwords(r.v[kb], p.v4 + row * (D / 2) + g * (D / 8));
         const uint8_t *s = p.scales + row * (D / 16) + (g * (D / 4)) / kBlock4;
@@ -224,58 +207,18 @@ __global__ __launch_bounds__(NW * kWave) void kv4_stream_kernel(Kv4AttnParams p)
 
     build_cumulative<NT>(p);
 
-    const int total = g_cum[p.B];
-    const int nw = min(p.num_wg, total);
-    auto share_start = [&](int u) { return (int)(((long long)min(u, nw) * total) / max(nw, 1)); };
-    auto share_of = [&](int t) { return (int)(((long long)(t + 1) * nw - 1) / total); };
-    const int start = share_start(w), end = share_start(w + 1);
+    const Shares sh(g_cum[p.B], p.num_wg);
+    const int start = sh.start_of(w), end = sh.start_of(w + 1);
 
     int pos = start;
     int anc_b = -1;
     if (start >= end && tid == 0) p.ws_desc[w * 4] = -1;
     while (pos < end) {
-        // ---- locate the unit holding tile `pos`
-        int lo = 0, hi = p.B - 1;
-        while (lo < hi) {
-            const int mid = (lo + hi + 1) >> 1;
-            if (g_cum[mid] <= pos) lo = mid; else hi = mid - 1;
-        }
-        const int b = lo;
-        const int L = g_len[b];
-        const int nodes = g_nn[b];
-        const int rows_b = nodes * p.G;
-        const Span sp = span_of(L, p);
-        const int ntp = (L + KT - 1) / KT - sp.gap;
-        auto real = [&](int t) { return t >= sp.ns ? t + sp.gap : t; };
-        const int C = p.setup_tiles;
-        const int per_g = tiles_per_head(ntp, rows_b, p);
-        int off = pos - g_cum[b];
-        const int g = off / per_g;
-        off -= g * per_g;
-        int rb = 0;
-        int ulen = ntp + tree_tiles_of_block(0, rows_b, p);
-        while (off >= C + ulen) {
-            off -= C + ulen;
-            ++rb;
-            ulen = ntp + tree_tiles_of_block(rb, rows_b, p);
-        }
-        const int v_end = min(C + ulen, off + (end - pos));
-        const int unit_real_start = pos - off + C;
-        const int t0 = max(off - C, 0);
-        if (pos == start && tid == 0) {
-            const int wf = share_of(unit_real_start);
-            const bool mine = unit_real_start < start && share_of(unit_real_start + ulen - 1) == w;
-            *reinterpret_cast<i32x4 *>(p.ws_desc + w * 4) =
-                mine ? i32x4{b, g, rb | (nodes << 8), wf * 2 + (unit_real_start <= share_start(wf) ? 0 : 1)}
-                     : i32x4{-1, 0, 0, 0};
-        }
-        pos += v_end - off;
-        const int t_end = v_end - C;
-        if (t_end <= t0) continue;
-        const bool complete = (t0 == 0 && t_end == ulen);
+        Piece pc;
+        if (!next_piece(p, sh, w, start, end, pos, pc)) continue;
+        const int b = pc.b, g = pc.g, rb = pc.rb, nodes = pc.nodes, rows_b = pc.rows_b, ntp = pc.ntp;
 
-        const bool edge = t_end > sp.ns && real(max(t0, sp.ns)) * KT < sp.lo0 + p.N - 1;
-        if ((t_end > ntp || edge) && anc_b != b) {
+        if (needs_paths(p, pc) && anc_b != b) {
             if (wave_u == 0) {
                 if (p.N <= kWave)
                     build_ancestor_masks_wave(p, lane < p.N ? p.parent[(size_t)b * p.N + lane] : -1);
@@ -305,52 +248,46 @@ __global__ __launch_bounds__(NW * kWave) void kv4_stream_kernel(Kv4AttnParams p)
         }
 
         // ---- this wave's tiles
-        const int tp_end = min(t_end, ntp);
+        const int tp_end = min(pc.t_end, ntp);
+        auto base_of = [&](int t) { return pc.real(t) * KT; };
         Raw4<D> raw;
         int ids[4];
-        int t = t0 + wave_u;
+        int t = pc.t0 + wave_u;
         if (t < tp_end) {
-            load_ids(p, b, real(t) * KT, c, ids);
-            load_raw<D>(p, g, real(t) * KT, L, sp, lane, ids, raw);
-            if (t + NW < tp_end) load_ids(p, b, real(t + NW) * KT, c, ids);
+            load_ids(p, b, base_of(t), c, ids);
+            load_raw<D>(p, pc, base_of(t), lane, ids, raw);
+            if (t + NW < tp_end) load_ids(p, b, base_of(t + NW), c, ids);
         }
         for (; t < tp_end; t += NW) {
-            const int base = real(t) * KT;
+            const int base = base_of(t);
             Raw4<D> cur = raw;
             if (t + NW < tp_end) {
-                load_raw<D>(p, g, real(t + NW) * KT, L, sp, lane, ids, raw);
-                if (t + 2 * NW < tp_end) load_ids(p, b, real(t + 2 * NW) * KT, c, ids);
+                load_raw<D>(p, pc, base_of(t + NW), lane, ids, raw);
+                if (t + 2 * NW < tp_end) load_ids(p, b, base_of(t + 2 * NW), c, ids);
             }
-            const bool masked = base + KT > L || !window_clear(sp, base, p.N);
+            const bool masked = base + KT > pc.L || !window_clear(pc.sp, base, p.N);
             if (__any(cur.live != 15u)) drop_dead(cur);
             stream_tile<D, NR>(
                 st, vtile, [&](int kb, int i) { return from4x8(cur.k[kb][i], scale4(cur.ks[kb])); },
                 [&](int kb, int i) { return from4x8(cur.v[kb][i], scale4(cur.vs[kb])); }, masked,
-                [&](int nr) {
-                    const int lim = L - base;
-                    unsigned long long x = lim >= KT ? ~0ull : (1ull << lim) - 1ull;
-                    if (!window_clear(sp, base, p.N)) x &= window_bits(sp, base, depth_of(g_anc[node[nr]]));
-                    return x;
-                },
-                p.scale_log2, lane);
+                [&](int nr) { return prefix_bits(p, pc, base, node[nr]); }, p.scale_log2, lane);
         }
-        for (; t < t_end; t += NW) {
+        for (; t < pc.t_end; t += NW) {
             // tree rows, in bf16; a slot past the sequence's nodes reads node 0's row
             const int j0 = (t - ntp) * KT;
-            auto row_of = [&](const uint16_t *from, int kb, int i) {
+            auto tree_row = [&](const uint16_t *from, int kb, int i) {
                 const int j = j0 + 16 * kb + c;
                 return *reinterpret_cast<const bf16x8 *>(
                     from + (((size_t)b * p.N + (j < nodes ? j : 0)) * p.Hkv + g) * D + g4 * (D / 4) + 8 * i);
             };
             stream_tile<D, NR>(
-                st, vtile, [&](int kb, int i) { return row_of(p.k_tree, kb, i); },
-                [&](int kb, int i) { return row_of(p.v_tree, kb, i); }, true,
-                [&](int nr) { return window_path(g_anc[node[nr]], t - ntp, L, p); }, p.scale_log2, lane);
+                st, vtile, [&](int kb, int i) { return tree_row(p.k_tree, kb, i); },
+                [&](int kb, int i) { return tree_row(p.v_tree, kb, i); }, true,
+                [&](int nr) { return window_path(g_anc[node[nr]], t - ntp, pc.L, p); }, p.scale_log2, lane);
         }
 
         // ---- the waves' (max, sum, O^T) meet in LDS and combine with the log-sum-exp rule;
         // thread (row, 8-column chunk) writes one 16-byte piece of the row
-        const int slot = w * 2 + (unit_real_start <= start ? 0 : 1);
         constexpr int kCh = D / 8;
         float *ow = reinterpret_cast<float *>(g_ring);                     // [NW][R][D]
         float *mlw = reinterpret_cast<float *>(g_anc_alt);                 // [NW][R][2]
@@ -394,7 +331,7 @@ __global__ __launch_bounds__(NW * kWave) void kv4_stream_kernel(Kv4AttnParams p)
             }
             const float inv = 1.f / lsum;
             const int ur = rb * R + r;
-            if (complete) {
+            if (pc.complete) {
                 bf16x8 o;
                 #pragma unroll
                 for (int e = 0; e < 8; ++e) o[e] = (__bf16)(acc[e] * inv);
@@ -421,27 +358,16 @@ __global__ __launch_bounds__(NW * kWave) void kv4_stream_kernel(Kv4AttnParams p)
                 f16x8 f;
                 #pragma unroll
                 for (int e = 0; e < 8; ++e) f[e] = (_Float16)(acc[e] * scaled);
-                *reinterpret_cast<f16x8 *>(p.ws_o + ((size_t)slot * p.rows_per_block + r) * D + ch * 8) = f;
+                *reinterpret_cast<f16x8 *>(p.ws_o + ((size_t)pc.slot * p.rows_per_block + r) * D + ch * 8) = f;
                 if (ch == 0)
-                    *reinterpret_cast<f32x4 *>(p.ws_ml + ((size_t)slot * p.rows_per_block + r) * 4) =
+                    *reinterpret_cast<f32x4 *>(p.ws_ml + ((size_t)pc.slot * p.rows_per_block + r) * 4) =
                         f32x4{none ? kNegInf : M * cs, none ? 0.f : lsum, none ? 1.f : unscale, 0.f};
             }
         }
         __syncthreads();                   // the next piece's V tiles and ancestor sets
     }
 
-    // Rows of padding nodes: zeros with lse -inf, a few nodes per workgroup.
-    if (p.num_nodes) {
-        const int chunks = p.Hq * D / 8;
-        for (int idx = w; idx < p.B * p.N; idx += p.num_wg) {
-            const int b = idx / p.N, i = idx - b * p.N;
-            if (i < g_nn[b]) continue;
-            u16x8 *op = reinterpret_cast<u16x8 *>(p.out + ((size_t)b * p.N + i) * p.Hq * D);
-            for (int ch = tid; ch < chunks; ch += NT) op[ch] = u16x8{0, 0, 0, 0, 0, 0, 0, 0};
-            if (p.lse)
-                for (int h = tid; h < p.Hq; h += NT) p.lse[((size_t)b * p.N + i) * p.Hq + h] = kNegInf;
-        }
-    }
+    clear_padding<D, NT>(p, w);
 }
 
 template <int D>
@@ -451,8 +377,7 @@ hipError_t launch_d(const Kv4AttnParams &p, hipStream_t s) {
     switch (p.rows_per_block) {
         case 16: e = go(kv4_stream_kernel<D, 8, 1>, 8); break;
         case 32: e = go(kv4_stream_kernel<D, 8, 2>, 8); break;
-        case 64: e = go(kv4_stream_kernel<D, 4, 4>, 4); break;
-        default: return hipErrorInvalidValue;
+        default: e = launch_kv4_wide(p, D, s);
     }
     if (e != hipSuccess || p.num_wg == 1) return e;
     constexpr int kRowsPerWg = 256 / (D / 8);

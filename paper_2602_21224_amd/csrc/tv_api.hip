@@ -345,14 +345,15 @@ void window_params(tv::WindowAttnParams &p, const uint16_t *q, const uint16_t *k
     p.window = window; p.sinks = sinks;
 }
 
-// Attention over a cache in 4 bits: one to four 16-row tiles per wave, rows beyond 64 in
-// blocks of 64.
-constexpr int kKv4SetupTiles = 4;
-constexpr int kKv4MinShareTiles = 8;
+// Attention over a cache in 4 bits: up to 32 rows per KV head wave by wave, more in blocks of
+// 128 or 256 rows.
+constexpr int kKv4StreamRows = 32;
+constexpr int kKv4StreamSetupTiles = 4;
+constexpr int kKv4StreamMinShareTiles = 8;
 
 AttnShape kv4_shape(int N, int Hq, int Hkv) {
     AttnShape s = attn_shape(N, Hq, Hkv);
-    s.rows_per_block = s.rows <= 16 ? 16 : s.rows <= 32 ? 32 : 64;
+    s.rows_per_block = s.rows <= 16 ? 16 : s.rows <= kKv4StreamRows ? 32 : s.rows <= 128 ? 128 : 256;
     s.row_blocks = (s.rows + s.rows_per_block - 1) / s.rows_per_block;
     s.tree_tiles_all = s.row_blocks * ((N + tv::kKeyTile - 1) / tv::kKeyTile);      // at most
     return s;
@@ -734,8 +735,10 @@ int tree_verify_attention_kv4(const uint16_t *q, const uint16_t *k_tree, const u
     const int max_wg = cu_count() * kWgPerCu;
     const AttnWorkspace ws = attn_workspace(s, D, max_wg, true);
     if (workspace_bytes < ws.total) return TV_ERR_WORKSPACE;
+    const bool stream_waves = s.rows <= kKv4StreamRows;
+    const int setup = stream_waves ? kKv4StreamSetupTiles : kSetupTiles;
     auto tiles_of = [&](long tiles) {
-        return (long)B * Hkv * ((long)s.row_blocks * (tiles + kKv4SetupTiles) + s.tree_tiles_all);
+        return (long)B * Hkv * ((long)s.row_blocks * (tiles + setup) + s.tree_tiles_all);
     };
     const long max_len = (long)max_pages * P;
     if (tiles_of((max_len + tv::kKeyTile - 1) / tv::kKeyTile) >= kMaxTiles) return TV_ERR_SHAPE;
@@ -745,11 +748,12 @@ int tree_verify_attention_kv4(const uint16_t *q, const uint16_t *k_tree, const u
     window_params(p, q, k_tree, v_tree, page_table, kv_len, parent, num_nodes, B, N, Hq, Hkv, D, P, max_pages, num_pages,
                   window, sinks, scale, out, lse, workspace, ws);
     p.k4 = k4; p.v4 = v4; p.scales = scales;
-    long num_wg = tiles_of(window_tiles(max_kv_len < max_len ? max_kv_len : max_len, window, sinks)) / kKv4MinShareTiles;
+    long num_wg = tiles_of(window_tiles(max_kv_len < max_len ? max_kv_len : max_len, window, sinks)) /
+                  (stream_waves ? kKv4StreamMinShareTiles : kMinShareTiles);
     if (num_wg < 1) num_wg = 1;
     if (num_wg > max_wg) num_wg = max_wg;
     p.rows_per_block = s.rows_per_block;
-    p.setup_tiles = kKv4SetupTiles;
+    p.setup_tiles = setup;
     p.num_wg = (int)num_wg;
     return tv::launch_kv4_attention(p, D, stream) == hipSuccess ? TV_OK : TV_ERR_HIP;
 }

@@ -250,6 +250,7 @@ hipError_t launch_accumulate_weights(const WeightParams &p, int head_dim, hipStr
 hipError_t launch_evict(EvictParams p, hipStream_t s);
 hipError_t launch_window_attention(const WindowAttnParams &p, int head_dim, int waves, hipStream_t s);
 hipError_t launch_kv4_attention(const Kv4AttnParams &p, int head_dim, hipStream_t s);
+hipError_t launch_kv4_wide(const Kv4AttnParams &p, int head_dim, hipStream_t s);   // the main kernel for many rows
 hipError_t launch_kv4_write(const Kv4WriteParams &p, int B, int head_dim, hipStream_t s);
 hipError_t launch_validate(const int32_t *page_table, const int32_t *kv_len,
                            const int32_t *parent, const int32_t *num_nodes, int B, int N, int P,
