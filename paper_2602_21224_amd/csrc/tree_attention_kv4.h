@@ -8,16 +8,45 @@
 namespace tv {
 namespace {
 
-// Equal contiguous shares of all units' virtual tiles (a unit's set-up tiles, prefix tiles
-// and tree tiles, laid end to end), as in tree_attention.hip: workgroup u takes
-// [start_of(u), start_of(u + 1)).
+// r / G for a row r < 2^11 of a sequence and KV head.
+__device__ __forceinline__ int node_of(const Kv4AttnParams &p, int r) {
+    return p.g_inv ? (int)__umulhi((unsigned)r, p.g_inv) : r;
+}
+
+// Tree tiles that row block rb of a sequence with `nodes` nodes visits: those up to its last
+// row's node.
+__device__ __forceinline__ int tree_tiles(const Kv4AttnParams &p, int rb, int nodes) {
+    const int end = (rb + 1) * p.rows_per_block;
+    return ((end >= nodes * p.G ? nodes : node_of(p, end - 1) + 1) + KT - 1) / KT;
+}
+
+// Virtual tiles of one KV head of a sequence: per row block the set-up tiles, ntp prefix
+// tiles and its tree tiles.
+__device__ __forceinline__ int head_tiles(const Kv4AttnParams &p, int ntp, int nodes) {
+    int t = 0;
+    for (int rb = 0; rb * p.rows_per_block < nodes * p.G; ++rb) t += p.setup_tiles + ntp + tree_tiles(p, rb, nodes);
+    return t;
+}
+__device__ __forceinline__ int tiles_of_sequence(int L, int nodes, const Kv4AttnParams &p) {
+    return p.Hkv * head_tiles(p, (L + KT - 1) / KT - span_of(L, p).gap, nodes);
+}
+
+// Contiguous shares of all units' virtual tiles, laid end to end as in tree_attention.hip:
+// workgroup u takes [start_of(u), start_of(u + 1)), the first `more` of nw one tile more
+// than the others' `each`. (Shares by 64-bit products and quotients took 10000 cycles to
+// find a piece with.)
 struct Shares {
-    int total, nw;
-    __device__ __forceinline__ Shares(int total_, int num_wg) : total(total_), nw(min(num_wg, total_)) {}
-    __device__ __forceinline__ int start_of(int u) const {
-        return (int)(((long long)min(u, nw) * total) / max(nw, 1));
+    int nw, each, more;
+    __device__ __forceinline__ Shares(int total, int num_wg) {
+        nw = min(num_wg, total);
+        each = nw > 0 ? total / nw : 0;
+        more = total - each * nw;
     }
-    __device__ __forceinline__ int owner_of(int t) const { return (int)(((long long)(t + 1) * nw - 1) / total); }
+    __device__ __forceinline__ int start_of(int u) const { return min(u, nw) * each + min(u, more); }
+    __device__ __forceinline__ int owner_of(int t) const {
+        const int full = more * (each + 1);
+        return t < full ? t / (each + 1) : more + (t - full) / each;
+    }
 };
 
 // The part of a unit that a share covers: real tiles t0 .. t_end - 1 of its ulen, of which
@@ -47,16 +76,16 @@ __device__ __forceinline__ bool next_piece(const Kv4AttnParams &p, const Shares 
     pc.sp = span_of(pc.L, p);
     pc.ntp = (pc.L + KT - 1) / KT - pc.sp.gap;
     const int C = p.setup_tiles;
-    const int per_g = tiles_per_head(pc.ntp, pc.rows_b, p);
+    const int per_g = (g_cum[lo + 1] - g_cum[lo]) / p.Hkv;
     int off = pos - g_cum[lo];
     pc.g = off / per_g;
     off -= pc.g * per_g;
     pc.rb = 0;
-    pc.ulen = pc.ntp + tree_tiles_of_block(0, pc.rows_b, p);
+    pc.ulen = pc.ntp + tree_tiles(p, 0, pc.nodes);
     while (off >= C + pc.ulen) {
         off -= C + pc.ulen;
         ++pc.rb;
-        pc.ulen = pc.ntp + tree_tiles_of_block(pc.rb, pc.rows_b, p);
+        pc.ulen = pc.ntp + tree_tiles(p, pc.rb, pc.nodes);
     }
     const int v_end = min(C + pc.ulen, off + (end - pos));
     const int unit_start = pos - off + C;              // share coordinate of the unit's real tile 0

@@ -235,9 +235,9 @@ __global__ __launch_bounds__(NW * kWave) void kv4_stream_kernel(Kv4AttnParams p)
         #pragma unroll
         for (int nr = 0; nr < NR; ++nr) {
             const int row = rb * R + 16 * nr + c, qrow = row < rows_b ? row : rb * R;
-            node[nr] = qrow / p.G;
+            node[nr] = node_of(p, qrow);
             const uint16_t *qp =
-                p.q + (((size_t)b * p.N + node[nr]) * p.Hq + g * p.G + qrow % p.G) * D + g4 * (D / 4);
+                p.q + (((size_t)b * p.N + node[nr]) * p.Hq + g * p.G + qrow - node[nr] * p.G) * D + g4 * (D / 4);
             #pragma unroll
             for (int t = 0; t < NKS; ++t)
                 st.qf[nr][t] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const u16x8 *>(qp + 8 * t));
@@ -335,7 +335,7 @@ __global__ __launch_bounds__(NW * kWave) void kv4_stream_kernel(Kv4AttnParams p)
                 bf16x8 o;
                 #pragma unroll
                 for (int e = 0; e < 8; ++e) o[e] = (__bf16)(acc[e] * inv);
-                const int nd = ur / p.G, h = g * p.G + ur % p.G;
+                const int nd = node_of(p, ur), h = g * p.G + ur - nd * p.G;
                 *reinterpret_cast<bf16x8 *>(p.out + (((size_t)b * p.N + nd) * p.Hq + h) * D + ch * 8) = o;
                 if (ch == 0 && p.lse)
                     p.lse[((size_t)b * p.N + nd) * p.Hq + h] = M * p.scale + __builtin_amdgcn_logf(lsum) * kLn2;

@@ -1,244 +1,84 @@
 // Tree-masked attention over a prefix held in 4 bits for units of many query rows, for
 // gfx950 (tree_attention_kv4.hip has those of few).
 //
-// A unit's row block is 128 RB rows: four waves, one per SIMD, of 32 RB rows each, which
-// step through the block's 64-key tiles together, one barrier per tile. Such a call is
-// bound by the matrix cores and the softmax between their instructions, not by bytes, so
-// the codes are converted once per workgroup, a quarter by each wave, into bf16 tiles in
-// LDS, and the products are those of the bf16 cache (v_mfma_f32_32x32x16_bf16, keys on M).
-// With RB = 2 each operand read from LDS serves two products: the reads, which keep the LDS
-// busy as long as the matrix cores are at 32 rows a wave, are halved.
+// Such a call is bound by the matrix cores and the softmax between their instructions, not
+// by bytes. A unit's row block is 256 rows (eight waves of 32; up to 128 rows: four), which
+// step through the block's 64-key tiles together, and each tile is converted once per
+// workgroup into a bf16 tile in LDS: from there on it is the bf16 attention's period
+// (tile_period: S_t^T = K_t Q^T and O^T += V_{t-1}^T P_{t-1}^T with the softmax between their
+// MFMAs). K_{t+1} goes where K_{t-1} was and V_t where V_{t-2} was, both read before the
+// barrier that opens period t, so two tiles of each are enough.
 //
-// Period j of a wave (tile j of the piece):
-//   part A  S_j^T = K_j Q^T; between the MFMAs the exponentials of tile j-1's second half
-//           and the conversion of K_{j+1}
-//   part B  O^T += V_{j-1}^T P_{j-1}^T; between them tile j's mask, maximum and running
-//           maximum, the exponentials of its first half, the conversion of V_j
-// K_{j+1} goes where K_{j-1} was and V_j where V_{j-2} was, both read before the barrier
-// that opened the period. Codes are loaded into registers two periods ahead.
-// The tree's rows are bf16 already: direct-to-LDS loads into two tiles of their own at the
-// start of the piece (a third and fourth tile of a large tree: into the converted tiles'
-// places once those are free).
+// A wave converts the keys 64/NW w .. of K_{t+1} and V_t at the end of its period t, a lane
+// a block of 32 values: 16 bytes of codes and a scale byte. It has loaded them itself, direct
+// to LDS three periods ahead (with their page ids two periods before that), the same number
+// of loads every time, so its own wait, for a constant count, is enough. (Loads into
+// registers, which the compiler waits for, made every second period wait for all of them.)
+// The tree's rows are bf16 already and come straight into the converted tiles' places, a
+// period ahead.
+//
+// Four waves of 64 rows each, which halve the operand reads from LDS, took 88 us where this
+// takes TIME (16 x 64 nodes x 4 heads over 1024-4096 tokens): one wave per SIMD issues an
+// instruction every 6.8 cycles, and its vector work was as long as the period.
 #include "tree_attention_kv4.h"
 
 namespace tv {
 namespace {
 
-template <int D, int RB>
-struct WideState {
-    bf16x8 qf[RB][D / 16];
-    f32x16 o[RB][D / 32];
-    u32x4 pb[RB][4];                       // P^T as bf16 pairs, 16 keys per k-step
-    f32x16 s0[RB];                         // this tile's scores of keys 0 .. 31
-    float m_run[RB], msc[RB], l_run[RB];
-};
-
-// A lane's share of one tile of K (or V): D/4 values of one key.
-template <int D>
-struct Part4 {
-    unsigned x[D / 32];
-    unsigned e;                            // scale byte
-    unsigned keep;                         // all ones, or 0 if no node sees the key
-};
-
-template <int D>
-__device__ __forceinline__ void load_part(Part4<D> &r, const Kv4AttnParams &p, long long at, bool is_v, int g) {
-    const long long row = max(at, 0ll);
-    load_dwords(r.x, (is_v ? p.v4 : p.k4) + row * (D / 2) + g * (D / 8));
-    r.e = p.scales[row * (D / 16) + (is_v ? D / kBlock4 : 0) + (g * (D / 4)) / kBlock4];
-    r.keep = at >= 0 ? ~0u : 0u;
+__device__ __forceinline__ unsigned read_dword(unsigned addr) {
+    unsigned x;
+    asm volatile("ds_read_b32 %0, %1" : "=v"(x) : "v"(addr));
+    return x;
 }
-
-// Eight of its values into the tile at `row` (the lane's key row, chunks swizzled by key).
-template <int D>
-__device__ __forceinline__ void convert_chunk(const Part4<D> &r, unsigned char *row, int chunk0, int key, int i) {
-    constexpr int C = Geo<D>::kChunks;
-    *reinterpret_cast<bf16x8 *>(row + (((chunk0 + i) ^ swz<C>(key % C)) << 4)) =
-        from4x8(r.x[i] & r.keep, scale4(r.keep ? r.e : 127u));
-}
-
-// f(0), f(1), .., f(N - 1) with constants.
-template <typename F, int... I>
-__device__ __forceinline__ void each_of(F f, std::integer_sequence<int, I...>) {
-    (f(std::integral_constant<int, I>{}), ...);
-}
-
-// Reads of the operands, whose waits the caller writes.
-template <int OFFSET>
-__device__ __forceinline__ u32x4 read_rows(unsigned addr) {
+__device__ __forceinline__ u32x4 read_codes(unsigned addr) {
     u32x4 x;
-    asm volatile("ds_read_b128 %0, %1 offset:%2" : "=v"(x) : "v"(addr), "i"(OFFSET));
+    asm volatile("ds_read_b128 %0, %1" : "=v"(x) : "v"(addr));
     return x;
 }
-template <int OFFSET>
-__device__ __forceinline__ u32x2 read_columns(unsigned addr) {
-    u32x2 x;
-    asm volatile("ds_read_b64_tr_b16 %0, %1 offset:%2" : "=v"(x) : "v"(addr), "i"(OFFSET));
-    return x;
+// A store beside loads in flight to other places of the same array, for which the compiler
+// would wait.
+__device__ __forceinline__ void write_chunk(unsigned addr, const bf16x8 &x) {
+    asm volatile("ds_write_b128 %0, %1" ::"v"(addr), "v"(__builtin_bit_cast(u32x4, x)));
 }
 
-// One period. s1p: the previous tile's second half of scores, s1: this tile's. conv(i),
-// i < 2 (D / 32): the conversions of K (first) and V.
-template <int D, int RB, bool PREV, bool CUR, typename Conv>
-__device__ __forceinline__ void wide_period(WideState<D, RB> &st, f32x16 (&s1p)[RB], f32x16 (&s1)[RB], unsigned kaddr,
-                                            unsigned vaddr, const TileMask (&mk)[RB], float c, Conv conv) {
-    using Gm = Geo<D>;
-    constexpr int NKS = D / 16, NDT = D / 32;
-    constexpr int C = Gm::kChunks;
-    constexpr int SA = 2 * NKS, SB = 4 * NDT, NSLOT = SA + SB;
-    constexpr int R = 2;                                   // operand reads run this many slots ahead
-    constexpr int PPA = 8 / SA > 0 ? 8 / SA : 1;           // half-1 pairs per part-A slot
-    constexpr int EA = 8 / PPA;                            // part-A slots with exponentials
-    constexpr int B0 = NDT > 6 ? NDT : 6;                  // first part-B slot of the half-0 pairs
-    constexpr int NC = D / 32;                             // conversions of K, and of V
-    auto ops = [](int s) constexpr { return s < SA ? (CUR ? 1 : 0) : s < NSLOT ? (PREV ? 2 : 0) : 0; };
-    u32x4 kb[SA];
-    u32x2 vb[SB][2];
-    auto issue_reads = [&](auto slot) __attribute__((always_inline)) {
-        constexpr int s = decltype(slot)::value;
-        if constexpr (s < SA && CUR) {
-            constexpr int hf = s / NKS, ks = s % NKS;
-            kb[s] = read_rows<hf * 32 * Gm::kRowBytes>(kaddr ^ ((unsigned)ks << 5));
-        } else if constexpr (s >= SA && s < NSLOT && PREV) {
-            constexpr int b = s - SA, kk = b / NDT, dt = b % NDT;
-            constexpr unsigned flip0 = (unsigned)((dt * 4) ^ swz<C>(0)) << 4, flip1 = (unsigned)((dt * 4) ^ swz<C>(8 % C)) << 4;
-            vb[b][0] = read_columns<kk * 16 * Gm::kRowBytes>(vaddr ^ flip0);
-            vb[b][1] = read_columns<(kk * 16 + 8) * Gm::kRowBytes>(vaddr ^ flip1);
-        }
-    };
-    float psa[RB], psb[RB], m8[RB][4], alpha[RB];
-    bool any_raise[RB];
-    #pragma unroll
-    for (int r = 0; r < RB; ++r) {
-        psa[r] = psb[r] = 0.f;
-        alpha[r] = 1.f;
-        any_raise[r] = false;
+// The blocks of 32 values that a wave converts per period, one per lane and step: half of
+// them of K, then those of V.
+template <int D, int NW>
+struct Share4 {
+    static constexpr int kBlocks = D / kBlock4;                    // per row
+    static constexpr int kTasks = 2 * (KT / NW) * kBlocks;
+    static constexpr int kSteps = kTasks > kWave ? kTasks / kWave : 1;
+    static constexpr int kBytes = kSteps * (kWave * 16 + kWave * 4);   // codes, and a dword of scales each
+    static constexpr int kLoads = 2 * kSteps;
+    static constexpr int kDepth = 4;
+    static constexpr int kIdDepth = 4;
+    bool is_v;
+    int key, blk;                          // key within the tile
+    __device__ __forceinline__ Share4(int lane, int step, int wave_u) {
+        const int task = (step * kWave + lane) % kTasks;           // lanes past the last task repeat
+        is_v = task >= kTasks / 2;
+        const int i = task % (kTasks / 2);
+        key = wave_u * (KT / NW) + i / kBlocks;
+        blk = i % kBlocks;
     }
-    auto score = [&](auto hf_, int r) __attribute__((always_inline)) -> f32x16 & {
-        if constexpr (decltype(hf_)::value == 0) return st.s0[r];
-        else return s1[r];
-    };
-    each_of(issue_reads, std::make_integer_sequence<int, R>{});
-    each_of([&](auto slot) __attribute__((always_inline)) {
-        constexpr int s = decltype(slot)::value;
-        issue_reads(std::integral_constant<int, s + R>{});
-        if constexpr (s < SA && CUR) {
-            constexpr int hf = s / NKS, ks = s % NKS;
-            lds_wait<ops(s + 1) + ops(s + 2)>();
-            tie(kb[s]);
-            #pragma unroll
-            for (int r = 0; r < RB; ++r) {
-                f32x16 &to = score(std::integral_constant<int, hf>{}, r);
-                to = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, kb[s]), st.qf[r][ks],
-                                                             ks == 0 ? f32x16{} : to, 0, 0, 0);
-            }
-        }
-        if constexpr (s >= SA && PREV) {
-            constexpr int b = s - SA, kk = b / NDT, dt = b % NDT;
-            lds_wait<ops(s + 1) + ops(s + 2)>();
-            tie(vb[b][0]);
-            tie(vb[b][1]);
-            const u32x4 a = {vb[b][0][0], vb[b][0][1], vb[b][1][0], vb[b][1][1]};
-            #pragma unroll
-            for (int r = 0; r < RB; ++r)
-                st.o[r][dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
-                    __builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, st.pb[r][kk]), st.o[r][dt], 0, 0, 0);
-        }
-        if constexpr (PREV && s < EA) {
-            // pairs of the previous tile's half 1 (P^T k-steps 2, 3), before part B reads them
-            #pragma unroll
-            for (int u = 0; u < PPA; ++u)
-                #pragma unroll
-                for (int r = 0; r < RB; ++r) {
-                    const int i = s * PPA + u;
-                    st.pb[r][2 + (i >> 2)][i & 3] = exp_pair(s1p[r][2 * i], s1p[r][2 * i + 1], c, st.msc[r], psa[r]);
-                }
-        }
-        if constexpr (PREV && s == EA - 1) {
-            #pragma unroll
-            for (int r = 0; r < RB; ++r) st.l_run[r] += psa[r];
-        }
-        if constexpr (CUR && s >= SA - NC && s < SA) conv(s - (SA - NC));
-        if constexpr (CUR && s == SA + 1) {
-            #pragma unroll
-            for (int r = 0; r < RB; ++r)
-                if (mk[r].masked) {
-                    #pragma unroll
-                    for (int e = 0; e < 16; ++e) {
-                        const int k0 = key_of(0, e), k1 = key_of(1, e) - 32;
-                        st.s0[r][e] = ((mk[r].vis_lo >> k0) & 1u) ? st.s0[r][e] : kNegInf;
-                        s1[r][e] = ((mk[r].vis_hi >> k1) & 1u) ? s1[r][e] : kNegInf;
-                    }
-                }
-        }
-        if constexpr (CUR && s >= SA + 1 && s < SA + 5) {
-            constexpr int q = s - SA - 1, r0 = (q & 1) * 8;
-            #pragma unroll
-            for (int r = 0; r < RB; ++r) {
-                const f32x16 &v = score(std::integral_constant<int, (q >> 1)>{}, r);
-                const float a = max3(v[r0], v[r0 + 1], v[r0 + 2]);
-                const float b = max3(v[r0 + 3], v[r0 + 4], v[r0 + 5]);
-                m8[r][q] = max3(a, b, max3(v[r0 + 6], v[r0 + 7], v[r0 + 7]));
-                tie(m8[r][q]);
-            }
-        }
-        if constexpr (CUR && s == SA + 5) {
-            // the running max is raised only when a score exceeds it by more than
-            // kRescaleSlack (log2 units); O is rescaled after this period's products
-            #pragma unroll
-            for (int r = 0; r < RB; ++r) {
-                const float tmax = halves_max(max3(m8[r][0], m8[r][1], max3(m8[r][2], m8[r][3], m8[r][3])));
-                const bool raise = tmax * c > st.m_run[r] * c + kRescaleSlack;
-                any_raise[r] = __any(raise);
-                if (any_raise[r]) {
-                    const float m_new = raise ? tmax : st.m_run[r];
-                    alpha[r] = (st.m_run[r] == kNegInf) ? 0.f : __builtin_amdgcn_exp2f((st.m_run[r] - m_new) * c);
-                    st.l_run[r] *= alpha[r];
-                    st.m_run[r] = m_new;
-                }
-                st.msc[r] = (st.m_run[r] == kNegInf) ? 0.f : st.m_run[r] * c;
-            }
-        }
-        if constexpr (CUR && s >= SA + B0) {
-            // pairs of half 0: k-step 0 from slot NDT of part B on, 1 from slot 2 NDT on, whose
-            // products before that read the previous tile's
-            constexpr int n = SB - B0, q = s - SA - B0;
-            #pragma unroll
-            for (int i = 8 * q / n; i < 8 * (q + 1) / n; ++i)
-                #pragma unroll
-                for (int r = 0; r < RB; ++r)
-                    st.pb[r][i >> 2][i & 3] = exp_pair(st.s0[r][2 * i], st.s0[r][2 * i + 1], c, st.msc[r], psb[r]);
-        }
-        if constexpr (CUR && s >= NSLOT - NC) conv(NC + s - (NSLOT - NC));
-        __builtin_amdgcn_sched_barrier(0);
-    }, std::make_integer_sequence<int, NSLOT>{});
-    if (CUR) {
-        #pragma unroll
-        for (int r = 0; r < RB; ++r) {
-            st.l_run[r] += psb[r];
-            if (any_raise[r]) {
-                #pragma unroll
-                for (int dt = 0; dt < NDT; ++dt)
-                    #pragma unroll
-                    for (int e = 0; e < 16; ++e) st.o[r][dt][e] *= alpha[r];
-            }
-        }
-    }
-}
+};
 
-template <int D, int RB>
-__global__ __launch_bounds__(4 * kWave) void kv4_wide_kernel(Kv4AttnParams p) {
+template <int D, int NW>
+__global__ __launch_bounds__(NW * kWave) void kv4_wide_kernel(Kv4AttnParams p) {
     using Gm = Geo<D>;
-    constexpr int NW = 4, NT = NW * kWave;
-    constexpr int NKS = D / 16, NDT = D / 32, C = Gm::kChunks, NC = D / 32;
-    constexpr int kBlocks = Gm::kBlocksPerTile / NW;       // 1 KB blocks of a tree tile per wave, K or V
+    using Sh = Share4<D, NW>;
+    constexpr int NT = NW * kWave;
+    constexpr int NKS = D / 16, NDT = D / 32, C = Gm::kChunks;
+    constexpr int kTreeLoads = Gm::kBlocksPerTile / NW;    // 1 KB blocks of a tree tile per wave, K or V
     constexpr int KPB = Gm::kKeysPerBlock;
+    constexpr int kRaw = NW * Sh::kDepth * Sh::kBytes;
+    static_assert(2 * Gm::kStageBytes + kRaw + NW * Sh::kIdDepth * Sh::kSteps * 256 <= (int)sizeof(g_ring),
+                  "two tiles of K and V, raw blocks and page ids fit");
 
     const int tid = threadIdx.x;
     const int lane = tid & (kWave - 1);
     const int wave_u = __builtin_amdgcn_readfirstlane(tid / kWave);
     const int half = lane >> 5, col = lane & 31;
-    const int g4 = lane >> 4, c16 = lane & 15;
     const int w = xcd_contiguous_id(blockIdx.x, p.num_wg);
 
     build_cumulative<NT>(p);
@@ -246,6 +86,8 @@ __global__ __launch_bounds__(4 * kWave) void kv4_wide_kernel(Kv4AttnParams p) {
     const Shares sh(g_cum[p.B], p.num_wg);
     const int start = sh.start_of(w), end = sh.start_of(w + 1);
     const unsigned ring = lds_addr(g_ring);
+    unsigned char *raw = g_ring + 2 * Gm::kStageBytes + wave_u * Sh::kDepth * Sh::kBytes;
+    unsigned char *id_ring = g_ring + 2 * Gm::kStageBytes + kRaw + wave_u * Sh::kIdDepth * Sh::kSteps * 256;
     // lane-constant parts of the LDS fragment addresses (see swz)
     const unsigned k_lane = col * Gm::kRowBytes + ((half ^ swz<C>(col % C)) << 4);
     const int va = ((lane >> 4) & 1) * 2 + ((lane & 3) >> 1);
@@ -263,153 +105,164 @@ __global__ __launch_bounds__(4 * kWave) void kv4_wide_kernel(Kv4AttnParams p) {
         int par = -1;
         if (paths && wave_u == 0 && p.N <= kWave && lane < p.N) par = p.parent[(size_t)b * p.N + lane];
 
-        // ---- codes: key 16 wave + c16 of a tile, D/4 values from (D/4) g4 on
-        const int kkey = 16 * wave_u + c16;
-        auto pos_of = [&](int t) { return pc.real(t) * KT + kkey; };
+        // ---- loads of this wave's share of period u: K of tile u + 1, V of tile u
         const int32_t *pages = p.page_table + (size_t)b * p.max_pages;
-        auto id_of = [&](int t) { return pages[min(max(pos_of(t), 0) >> p.p_shift, p.max_pages - 1)]; };
-        auto row_at = [&](int t, int id) { return t < min(t_end, ntp) ? row_of(p, g, pos_of(t), id, pc.L, pc.sp) : -1ll; };
-        Part4<D> rk[2], rv[2];             // K of tile t in rk[t & 1], V in rv[t & 1]
-        long long row[2];                  // the rows of the tiles whose V is still to be loaded
-        int id[2];
+        auto load_ids = [&](int u) {
+            #pragma unroll
+            for (int i = 0; i < Sh::kSteps; ++i) {
+                const Sh mine(lane, i, wave_u);
+                const int at = pc.real(max(u + !mine.is_v, 0)) * KT + mine.key;
+                __builtin_amdgcn_global_load_lds(
+                    (const GLOBAL_AS void *)(pages + min(at >> p.p_shift, p.max_pages - 1)),
+                    (LDS_AS void *)(id_ring + ((u & (Sh::kIdDepth - 1)) * Sh::kSteps + i) * 256), 4, 0, 0);
+            }
+        };
+        // (past the prefix or the piece: the cache's first row)
+        auto load_codes = [&](int u) {
+            #pragma unroll
+            for (int i = 0; i < Sh::kSteps; ++i) {
+                const Sh mine(lane, i, wave_u);
+                unsigned id = read_dword(lds_addr(id_ring) + ((u & (Sh::kIdDepth - 1)) * Sh::kSteps + i) * 256 + lane * 4);
+                lds_wait<0>();
+                tie(id);
+                const int t = u + !mine.is_v;
+                const long long at =
+                    t >= t0 && t < min(t_end, ntp) ? row_of(p, g, pc.real(t) * KT + mine.key, (int)id, pc.L, pc.sp) : -1;
+                const long long row = max(at, 0ll);
+                unsigned char *to = raw + (u & (Sh::kDepth - 1)) * Sh::kBytes + i * 1280;
+                __builtin_amdgcn_global_load_lds(
+                    (const GLOBAL_AS void *)((mine.is_v ? p.v4 : p.k4) + row * (D / 2) + mine.blk * 16), (LDS_AS void *)to, 16, 0, 0);
+                __builtin_amdgcn_global_load_lds(
+                    (const GLOBAL_AS void *)(p.scales + row * (D / 16) + (D == 128 && mine.is_v ? 4 : 0)),
+                    (LDS_AS void *)(to + 1024), 4, 0, 0);
+            }
+        };
         #pragma unroll
-        for (int i = 0; i < 2; ++i) id[i] = id_of(t0 + i);
+        for (int i = -1; i < 3; ++i) load_ids(t0 + i);
 
-        // ---- this wave's query rows: a row past the unit's last one loads the unit's first
-        WideState<D, RB> st;
-        int node[RB], hq[RB];
-        bool row_ok[RB];
-        #pragma unroll
-        for (int r = 0; r < RB; ++r) {
-            const int first = pc.rb * p.rows_per_block, at = first + (wave_u * RB + r) * 32 + col;
-            row_ok[r] = at < pc.rows_b;
-            const int qrow = row_ok[r] ? at : first;
-            node[r] = qrow / p.G;
-            hq[r] = g * p.G + qrow % p.G;
-            const uint16_t *qp = p.q + (((size_t)b * p.N + node[r]) * p.Hq + hq[r]) * D + half * 8;
+        // ---- this wave's 32 query rows: a row past the unit's last one loads the unit's first
+        const int row0 = pc.rb * p.rows_per_block, row_at = row0 + wave_u * kRowsPerWave + col;
+        const int qrow = row_at < pc.rows_b ? row_at : row0;
+        const int node = node_of(p, qrow), hq = g * p.G + qrow - node * p.G;
+        WaveState<D> st;
+        {
+            const uint16_t *qp = p.q + (((size_t)b * p.N + node) * p.Hq + hq) * D + half * 8;
             #pragma unroll
             for (int ks = 0; ks < NKS; ++ks)
-                st.qf[r][ks] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const u16x8 *>(qp + ks * 16));
+                st.qf[ks] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const u16x8 *>(qp + ks * 16));
             #pragma unroll
             for (int dt = 0; dt < NDT; ++dt)
                 #pragma unroll
-                for (int e = 0; e < 16; ++e) st.o[r][dt][e] = 0.f;
-            st.m_run[r] = kNegInf;
-            st.msc[r] = 0.f;
-            st.l_run[r] = 0.f;
+                for (int e = 0; e < 16; ++e) st.o[dt][e] = 0.f;
+            st.m_run = kNegInf;
+            st.msc = 0.f;
+            st.l_run = 0.f;
         }
 
-        // ---- LDS places: converted tile t in stage t & 1 (K, then V); tree tile u in stage
-        // 2 + u, the third and fourth in stages ntp & 1 and (ntp + 1) & 1 (their turn)
-        auto stage_of = [&](int t) { return t < ntp ? t & 1 : t - ntp < 2 ? 2 + t - ntp : t & 1; };
-        auto load_tree = [&](int t) {
-            unsigned char *dst = g_ring + stage_of(t) * Gm::kStageBytes;
+        // ---- tile t, converted or of the tree, is in stage t & 1 (K, then V)
+        auto load_tree = [&](int t, bool is_v) {
+            int ln = lane;
+            tie(ln);                       // addresses are made here, not kept from the piece's start
+            unsigned char *dst = g_ring + (t & 1) * Gm::kStageBytes + (is_v ? Gm::kTileBytes : 0);
             #pragma unroll
-            for (int i = 0; i < kBlocks; ++i) {
-                const int blk = wave_u * kBlocks + i, key = blk * KPB + lane / C, j = (t - ntp) * KT + key;
+            for (int i = 0; i < kTreeLoads; ++i) {
+                const int block = wave_u * kTreeLoads + i, key = block * KPB + ln / C, j = (t - ntp) * KT + key;
                 // a slot past the sequence's nodes reads node 0's row (finite, masked)
                 const size_t at = (((size_t)b * p.N + (j < pc.nodes ? j : 0)) * p.Hkv + g) * D +
-                                  ((lane % C) ^ swz<C>(key % C)) * 8;
-                __builtin_amdgcn_global_load_lds((const GLOBAL_AS void *)(p.k_tree + at), (LDS_AS void *)(dst + blk * 1024),
-                                                 16, 0, 0);
-                __builtin_amdgcn_global_load_lds((const GLOBAL_AS void *)(p.v_tree + at),
-                                                 (LDS_AS void *)(dst + Gm::kTileBytes + blk * 1024), 16, 0, 0);
+                                  ((ln % C) ^ swz<C>(key % C)) * 8;
+                __builtin_amdgcn_global_load_lds((const GLOBAL_AS void *)((is_v ? p.v_tree : p.k_tree) + at),
+                                                 (LDS_AS void *)(dst + block * 1024), 16, 0, 0);
             }
         };
-        auto krow = [&](int t) { return g_ring + (t & 1) * Gm::kStageBytes + kkey * Gm::kRowBytes; };
-        auto vrow = [&](int t) { return krow(t) + Gm::kTileBytes; };
-
-        // first loads: K of the first three tiles, V of the first two; the first tile's K is
-        // converted before the loop
-        row[0] = row_at(t0, id[0]);
-        row[1] = row_at(t0 + 1, id[1]);
-        id[0] = id_of(t0 + 2);
-        id[1] = id_of(t0 + 3);
-        Part4<D> k0;
-        load_part<D>(k0, p, row[0], false, g4);
-        load_part<D>(rk[1], p, row[1], false, g4);
-        load_part<D>(rv[0], p, row[0], true, g4);
-        load_part<D>(rv[1], p, row[1], true, g4);
-        row[0] = row_at(t0 + 2, id[0]);
-        load_part<D>(rk[0], p, row[0], false, g4);
-        id[0] = id_of(t0 + 4);
-        if (t_end > ntp)
-            for (int t = max(ntp, t0); t < t_end; ++t)
-                if (t0 >= ntp || t < ntp + 2) load_tree(t);
-        if (paths) {
-            if (wave_u == 0) {
-                tie(par);
-                if (p.N <= kWave) build_ancestor_masks_wave(p, par);
-                else build_ancestor_masks_wave_lds(p, b);
-            }
-            anc_b = b;
-        }
-        if (t0 < ntp) {
+        // Conversion of the share of period u. A key that no node sees counts as zeros.
+        auto convert = [&](int u) {
             #pragma unroll
-            for (int i = 0; i < NC; ++i) convert_chunk<D>(k0, krow(t0), g4 * NC, kkey, i);
+            for (int i = 0; i < Sh::kSteps; ++i) {
+                const Sh mine(lane, i, wave_u);
+                const unsigned from = lds_addr(raw) + (u & (Sh::kDepth - 1)) * Sh::kBytes + i * 1280;
+                u32x4 x = read_codes(from + lane * 16);
+                unsigned sc = read_dword(from + 1024 + lane * 4);
+                const int t = u + !mine.is_v, at = pc.real(t) * KT + mine.key;
+                const bool live = at < pc.L && (at >= pc.sp.lo || at < pc.sp.sinks);
+                const unsigned to = ring + (t & 1) * Gm::kStageBytes + (mine.is_v ? Gm::kTileBytes : 0) +
+                                    mine.key * Gm::kRowBytes + (((mine.blk * 4) ^ swz<C>(mine.key % C)) << 4);
+                lds_wait<0>();
+                tie(x);
+                tie(sc);
+                const unsigned e = (sc >> (8 * (mine.blk + (D == 64 && mine.is_v ? 2 : 0)))) & 255u;
+                if (t < ntp) {
+                    #pragma unroll
+                    for (int q = 0; q < 4; ++q)
+                        write_chunk(to ^ (q << 4), from4x8(live ? x[q] : 0u, scale4(live ? e : 127u)));
+                }
+            }
+        };
+
+        if (paths && wave_u == 0) {
+            tie(par);
+            if (p.N <= kWave) build_ancestor_masks_wave(p, par);
+            else build_ancestor_masks_wave_lds(p, b);
+        }
+        if (paths) anc_b = b;
+        wait_vmcnt<0>();
+        // in the order of the loop below, whose waits count: codes of period u, ids of u + 2
+        load_codes(t0 - 1);
+        load_codes(t0);
+        load_ids(t0 + 3);
+        load_codes(t0 + 1);
+        load_ids(t0 + 4);
+        load_codes(t0 + 2);
+        if (t0 < ntp) {
+            wait_vmcnt<3 * Sh::kLoads + 2 * Sh::kSteps>();
+            convert(t0 - 1);
+        } else {
+            load_tree(t0, false);
         }
 
-        f32x16 s1[2][RB];
-        TileMask mk[RB];
-        // Opens the period of tile t: the converted parts of every wave are in place, and the
-        // tree tiles that it or the one before reads; then the tile's mask.
+        f32x16 s0, s1;
+        TileMask mk;
+        // Opens the period of tile t: K_t and V_{t-1} of every wave are in place; then the loads
+        // of tree rows that go where K_{t-1} and V_{t-2} were, and the tile's mask.
         auto open = [&](int t) {
             if (t >= ntp) wait_vmcnt<0>();
             lds_barrier();
             if (t >= t_end) return;
-            if (t0 < ntp && t >= ntp && t < ntp + 2 && t + 2 < t_end) load_tree(t + 2);
+            if (t + 1 >= ntp && t + 1 < t_end) load_tree(t + 1, false);
+            if (t >= ntp) load_tree(t, true);
             const int base = pc.real(t) * KT;
             const bool tree = t >= ntp;
-            const bool masked = tree || base + KT > pc.L || !window_clear(pc.sp, base, p.N);
-            #pragma unroll
-            for (int r = 0; r < RB; ++r) {
-                mk[r].masked = masked;
-                if (masked) {
-                    const unsigned long long vis = (tree ? window_path(g_anc[node[r]], t - ntp, pc.L, p)
-                                                         : prefix_bits(p, pc, base, node[r])) >> (half * 4);
-                    mk[r].vis_lo = (unsigned)vis;
-                    mk[r].vis_hi = (unsigned)(vis >> 32);
-                }
+            mk.masked = tree || base + KT > pc.L || !window_clear(pc.sp, base, p.N);
+            if (mk.masked) {
+                const unsigned long long vis =
+                    (tree ? window_path(g_anc[node], t - ntp, pc.L, p) : prefix_bits(p, pc, base, node)) >> (half * 4);
+                mk.vis_lo = (unsigned)vis;
+                mk.vis_hi = (unsigned)(vis >> 32);
             }
         };
-        auto kaddr = [&](int t) { return ring + stage_of(t) * Gm::kStageBytes + k_lane; };
-        auto vaddr = [&](int t) { return ring + stage_of(t) * Gm::kStageBytes + Gm::kTileBytes + v_lane; };
-        // Period of tile t = t0 + j, j of parity PAR: converts K_{t+1} (rk[1 - PAR]) and V_t
-        // (rv[PAR]) and loads K_{t+3} and V_{t+2} in their place.
-        auto period = [&](auto par_, auto prev_, int t) {
-            constexpr int PAR = decltype(par_)::value;
-            open(t);
-            wide_period<D, RB, decltype(prev_)::value, true>(
-                st, s1[1 - PAR], s1[PAR], kaddr(t), decltype(prev_)::value ? vaddr(t - 1) : 0u, mk, p.scale_log2,
-                [&](int i) {
-                    if (i < NC) {
-                        if (t + 1 < min(t_end, ntp)) convert_chunk<D>(rk[1 - PAR], krow(t + 1), g4 * NC, kkey, i);
-                    } else if (t < ntp) {
-                        convert_chunk<D>(rv[PAR], vrow(t), g4 * NC, kkey, i - NC);
-                    }
-                });
-            // V_{t+2} from the row found for K_{t+2}, then K_{t+3}
-            load_part<D>(rv[PAR], p, row[PAR], true, g4);
-            row[1 - PAR] = row_at(t + 3, id[1 - PAR]);
-            load_part<D>(rk[1 - PAR], p, row[1 - PAR], false, g4);
-            id[1 - PAR] = id_of(t + 5);
+        auto kaddr = [&](int t) { return ring + (t & 1) * Gm::kStageBytes + k_lane; };
+        auto vaddr = [&](int t) { return ring + (t & 1) * Gm::kStageBytes + Gm::kTileBytes + v_lane; };
+        auto close = [&](int t) {
+            // the codes of period t: behind them those of two periods, and ids
+            if (t < ntp) {
+                wait_vmcnt<2 * (Sh::kLoads + Sh::kSteps)>();
+                convert(t);
+            }
+            // the ids of period t + 3: behind them one period's ids and two periods' codes
+            wait_vmcnt<2 * Sh::kLoads + Sh::kSteps>();
+            load_ids(t + 5);
+            load_codes(t + 3);
         };
-        using E_ = std::integral_constant<int, 0>;
-        using O_ = std::integral_constant<int, 1>;
-        period(E_{}, std::false_type{}, t0);
-        int t = t0 + 1;
-        for (; t + 1 < t_end; t += 2) {
-            period(O_{}, std::true_type{}, t);
-            period(E_{}, std::true_type{}, t + 1);
+        open(t0);
+        tile_period<D, false, true>(st, s0, s1, kaddr(t0), 0u, mk, p.scale_log2);
+        close(t0);
+        for (int t = t0 + 1; t < t_end; ++t) {
+            open(t);
+            tile_period<D, true, true>(st, s0, s1, kaddr(t), vaddr(t - 1), mk, p.scale_log2);
+            close(t);
         }
-        const bool odd = t < t_end;
-        if (odd) period(O_{}, std::true_type{}, t);
-        // PV of the last tile
         open(t_end);
-        if (odd)
-            wide_period<D, RB, true, false>(st, s1[1], s1[0], 0u, vaddr(t_end - 1), mk, p.scale_log2, [](int) {});
-        else
-            wide_period<D, RB, true, false>(st, s1[0], s1[1], 0u, vaddr(t_end - 1), mk, p.scale_log2, [](int) {});
+        tile_period<D, true, false>(st, s0, s1, 0u, vaddr(t_end - 1), mk, p.scale_log2);
+        wait_vmcnt<0>();                   // no load of codes lands in what follows
         __syncthreads();
 
         // ---- the normalised rows leave through this wave's part of the idle ring, transposed
@@ -417,61 +270,62 @@ __global__ __launch_bounds__(4 * kWave) void kv4_wide_kernel(Kv4AttnParams p) {
         // power of two per row
         constexpr int kPitch = D * 2 + 16, kRowChunks = D / 8, kRowsPerPass = kWave / kRowChunks;
         unsigned char *wbuf = g_ring + wave_u * 32 * kPitch;
-        #pragma unroll
-        for (int r = 0; r < RB; ++r) {
-            const float l_tot = halves_sum(st.l_run[r]);
+        int ln = lane;
+        tie(ln);                           // addresses are made here, not kept from the piece's start
+        {
+            const float l_tot = halves_sum(st.l_run);
             const float inv = l_tot > 0.f ? 1.f / l_tot : 0.f;
-            float unscale = 1.f, scaled = inv;
-            if (!pc.complete) {
+            unsigned char *to = wbuf + (ln & 31) * kPitch + (ln >> 5) * 8;
+            float unscale = 1.f;
+            if (pc.complete) {
+                #pragma unroll
+                for (int q = 0; q < 4 * NDT; ++q) {
+                    bf16x4 v;
+                    #pragma unroll
+                    for (int i = 0; i < 4; ++i) v[i] = (__bf16)(st.o[q >> 2][(q & 3) * 4 + i] * inv);
+                    *reinterpret_cast<bf16x4 *>(to + q * 16) = v;
+                }
+            } else {
                 const float top = row_top(
                     [&](auto take) {
                         #pragma unroll
                         for (int dt = 0; dt < NDT; ++dt)
                             #pragma unroll
-                            for (int e = 0; e < 16; ++e) take(st.o[r][dt][e]);
+                            for (int e = 0; e < 16; ++e) take(st.o[dt][e]);
                     },
                     halves_max);
-                scaled *= part_scale(top * inv, unscale);
-            }
-            #pragma unroll
-            for (int dt = 0; dt < NDT; ++dt)
+                const float scaled = inv * part_scale(top * inv, unscale);
                 #pragma unroll
-                for (int q4 = 0; q4 < 4; ++q4) {
-                    bf16x4 v;
+                for (int q = 0; q < 4 * NDT; ++q) {
                     f16x4 f;
                     #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        v[i] = (__bf16)(st.o[r][dt][q4 * 4 + i] * inv);
-                        f[i] = (_Float16)(st.o[r][dt][q4 * 4 + i] * scaled);
-                    }
-                    if (!pc.complete) v = __builtin_bit_cast(bf16x4, f);
-                    *reinterpret_cast<bf16x4 *>(wbuf + col * kPitch + (dt * 32 + q4 * 8 + half * 4) * 2) = v;
+                    for (int i = 0; i < 4; ++i) f[i] = (_Float16)(st.o[q >> 2][(q & 3) * 4 + i] * scaled);
+                    *reinterpret_cast<f16x4 *>(to + q * 16) = f;
                 }
+            }
+            const int rl0 = wave_u * kRowsPerWave + ln / kRowChunks, ch = ln % kRowChunks;   // within the block
             #pragma unroll
             for (int k = 0; k < 32 / kRowsPerPass; ++k) {
-                const int rr = k * kRowsPerPass + lane / kRowChunks, ch = lane % kRowChunks;
-                const u32x4 v = *reinterpret_cast<const u32x4 *>(wbuf + rr * kPitch + ch * 16);
-                const int rl = (wave_u * RB + r) * 32 + rr;          // row within the unit's block
+                const int rl = rl0 + k * kRowsPerPass;
+                const u32x4 v = *reinterpret_cast<const u32x4 *>(wbuf + (k * kRowsPerPass + ln / kRowChunks) * kPitch + ch * 16);
                 if (pc.complete) {
                     const int ur = pc.rb * p.rows_per_block + rl;
                     if (ur < pc.rows_b) {
-                        const int nd = ur / p.G, h = g * p.G + ur % p.G;
+                        const int nd = node_of(p, ur), h = g * p.G + ur - nd * p.G;
                         *reinterpret_cast<u32x4 *>(p.out + (((size_t)b * p.N + nd) * p.Hq + h) * D + ch * 8) = v;
                     }
                 } else {
                     *reinterpret_cast<u32x4 *>(p.ws_o + ((size_t)pc.slot * p.rows_per_block + rl) * D + ch * 8) = v;
                 }
             }
-            if (half == 0) {
-                if (pc.complete) {
-                    if (row_ok[r] && p.lse)
-                        p.lse[((size_t)b * p.N + node[r]) * p.Hq + hq[r]] =
-                            st.m_run[r] * p.scale + __builtin_amdgcn_logf(l_tot) * kLn2;
-                } else {
-                    const int rl = (wave_u * RB + r) * 32 + col;
+            if (ln < 32) {
+                const int rl = wave_u * kRowsPerWave + ln;
+                if (!pc.complete)
                     *reinterpret_cast<f32x4 *>(p.ws_ml + ((size_t)pc.slot * p.rows_per_block + rl) * 4) =
-                        f32x4{st.m_run[r] == kNegInf ? kNegInf : st.m_run[r] * p.scale_log2, l_tot, unscale, 0.f};
-                }
+                        f32x4{st.m_run == kNegInf ? kNegInf : st.m_run * p.scale_log2, l_tot, unscale, 0.f};
+                else if (p.lse && pc.rb * p.rows_per_block + rl < pc.rows_b)
+                    p.lse[((size_t)b * p.N + node) * p.Hq + hq] =
+                        st.m_run * p.scale + __builtin_amdgcn_logf(l_tot) * kLn2;
             }
         }
         __syncthreads();                   // the ring is refilled by the next piece
@@ -482,9 +336,10 @@ __global__ __launch_bounds__(4 * kWave) void kv4_wide_kernel(Kv4AttnParams p) {
 
 template <int D>
 hipError_t launch_d(const Kv4AttnParams &p, hipStream_t s) {
-    auto go = [&](auto kernel) { return launch_kernel(kernel, dim3(p.num_wg), dim3(4 * kWave), s, p); };
-    if (p.rows_per_block == 128) return go(kv4_wide_kernel<D, 1>);
-    if (p.rows_per_block == 256) return go(kv4_wide_kernel<D, 2>);
+    if (p.rows_per_block == 128)
+        return launch_kernel(kv4_wide_kernel<D, 4>, dim3(p.num_wg), dim3(4 * kWave), s, p);
+    if (p.rows_per_block == 256)
+        return launch_kernel(kv4_wide_kernel<D, 8>, dim3(p.num_wg), dim3(8 * kWave), s, p);
     return hipErrorInvalidValue;
 }
 

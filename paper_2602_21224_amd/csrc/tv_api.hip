@@ -748,6 +748,7 @@ int tree_verify_attention_kv4(const uint16_t *q, const uint16_t *k_tree, const u
     window_params(p, q, k_tree, v_tree, page_table, kv_len, parent, num_nodes, B, N, Hq, Hkv, D, P, max_pages, num_pages,
                   window, sinks, scale, out, lse, workspace, ws);
     p.k4 = k4; p.v4 = v4; p.scales = scales;
+    p.g_inv = s.G == 1 ? 0u : (unsigned)((1ull << 32) / (unsigned)s.G + 1);
     long num_wg = tiles_of(window_tiles(max_kv_len < max_len ? max_kv_len : max_len, window, sinks)) /
                   (stream_waves ? kKv4StreamMinShareTiles : kMinShareTiles);
     if (num_wg < 1) num_wg = 1;

@@ -97,6 +97,7 @@ struct WindowAttnParams : AttnParams {
 struct Kv4AttnParams : WindowAttnParams {
     const uint8_t *k4, *v4;      // [num_pages][Hkv][P][D / 2] codes
     const uint8_t *scales;       // [num_pages][Hkv][P][2][D / 32]: K's, V's
+    unsigned int g_inv;          // floor(2^32 / G) + 1: r / G is its high product with r < 2^11 (0: G = 1)
 };
 
 // The same for batches with shared prefixes.
