@@ -11,9 +11,11 @@
 //
 // A wave converts the keys 64/NW w .. of K_{t+1} and V_t at the end of its period t, a lane
 // a block of 32 values: 16 bytes of codes and a scale byte. It has loaded them itself, direct
-// to LDS three periods ahead (with their page ids two periods before that), the same number
-// of loads every time, so its own wait, for a constant count, is enough. (Loads into
-// registers, which the compiler waits for, made every second period wait for all of them.)
+// to LDS three periods ahead, the same number of loads every time, so its own wait, for a
+// constant count, is enough. (Loads into registers, which the compiler waits for, made every
+// second period wait for all of them.) Its keys of a tile lie in one page, whose id is a
+// scalar load; with smaller pages (SMALL) every lane has its own, by a direct-to-LDS load
+// two periods before the codes.
 // The tree's rows are bf16 already and come straight into the converted tiles' places, a
 // period ahead.
 //
@@ -53,17 +55,17 @@ struct Share4 {
     static constexpr int kDepth = 4;
     static constexpr int kIdDepth = 4;
     bool is_v;
-    int key, blk;                          // key within the tile
-    __device__ __forceinline__ Share4(int lane, int step, int wave_u) {
+    int key, blk;                          // key within the wave's
+    __device__ __forceinline__ Share4(int lane, int step) {
         const int task = (step * kWave + lane) % kTasks;           // lanes past the last task repeat
         is_v = task >= kTasks / 2;
         const int i = task % (kTasks / 2);
-        key = wave_u * (KT / NW) + i / kBlocks;
+        key = i / kBlocks;
         blk = i % kBlocks;
     }
 };
 
-template <int D, int NW>
+template <int D, int NW, bool SMALL>
 __global__ __launch_bounds__(NW * kWave) void kv4_wide_kernel(Kv4AttnParams p) {
     using Gm = Geo<D>;
     using Sh = Share4<D, NW>;
@@ -71,6 +73,8 @@ __global__ __launch_bounds__(NW * kWave) void kv4_wide_kernel(Kv4AttnParams p) {
     constexpr int NKS = D / 16, NDT = D / 32, C = Gm::kChunks;
     constexpr int kTreeLoads = Gm::kBlocksPerTile / NW;    // 1 KB blocks of a tree tile per wave, K or V
     constexpr int KPB = Gm::kKeysPerBlock;
+    constexpr int KPW = KT / NW;                           // keys of a tile that a wave converts
+    constexpr int L4 = Sh::kLoads, LID = SMALL ? Sh::kSteps : 0;   // its loads per period: codes, ids
     constexpr int kRaw = NW * Sh::kDepth * Sh::kBytes;
     static_assert(2 * Gm::kStageBytes + kRaw + NW * Sh::kIdDepth * Sh::kSteps * 256 <= (int)sizeof(g_ring),
                   "two tiles of K and V, raw blocks and page ids fit");
@@ -105,40 +109,69 @@ __global__ __launch_bounds__(NW * kWave) void kv4_wide_kernel(Kv4AttnParams p) {
         int par = -1;
         if (paths && wave_u == 0 && p.N <= kWave && lane < p.N) par = p.parent[(size_t)b * p.N + lane];
 
-        // ---- loads of this wave's share of period u: K of tile u + 1, V of tile u
+        // ---- loads of this wave's share of period u: K of tile u + 1, V of tile u (past the
+        // prefix or the piece, or without a page: the cache's first row)
         const int32_t *pages = p.page_table + (size_t)b * p.max_pages;
+        const int tp_end = min(t_end, ntp);
+        auto page_at = [&](int at) { return min(max(at, 0) >> p.p_shift, p.max_pages - 1); };
         auto load_ids = [&](int u) {
             #pragma unroll
             for (int i = 0; i < Sh::kSteps; ++i) {
-                const Sh mine(lane, i, wave_u);
-                const int at = pc.real(max(u + !mine.is_v, 0)) * KT + mine.key;
+                const Sh mine(lane, i);
+                const int at = pc.real(u + !mine.is_v) * KT + wave_u * KPW + mine.key;
                 __builtin_amdgcn_global_load_lds(
-                    (const GLOBAL_AS void *)(pages + min(at >> p.p_shift, p.max_pages - 1)),
+                    (const GLOBAL_AS void *)(pages + page_at(at)),
                     (LDS_AS void *)(id_ring + ((u & (Sh::kIdDepth - 1)) * Sh::kSteps + i) * 256), 4, 0, 0);
             }
         };
-        // (past the prefix or the piece: the cache's first row)
+        auto id_of = [&](int t) { return ((const CONST_AS int32_t *)pages)[page_at(pc.real(t) * KT + wave_u * KPW)]; };
+        // first row of the wave's keys of tile t on page id
+        auto first_row = [&](int t, int id) {
+            const int at = pc.real(t) * KT + wave_u * KPW;
+            const long long row = (((long long)(unsigned)id * (unsigned)p.Hkv + (unsigned)g) << p.p_shift) + (at & (p.P - 1));
+            return t >= t0 && t < tp_end && (unsigned)id < (unsigned)p.num_pages ? row : 0ll;
+        };
+        auto load_from = [&](int u, int i, const uint8_t *codes, const uint8_t *scales) {
+            unsigned char *to = raw + (u & (Sh::kDepth - 1)) * Sh::kBytes + i * 1280;
+            __builtin_amdgcn_global_load_lds((const GLOBAL_AS void *)codes, (LDS_AS void *)to, 16, 0, 0);
+            __builtin_amdgcn_global_load_lds((const GLOBAL_AS void *)scales, (LDS_AS void *)(to + 1024), 4, 0, 0);
+        };
+        long long row_v = 0;               // of the tile whose K was loaded last
+        int id_k = 0;                      // page id of the next one
         auto load_codes = [&](int u) {
-            #pragma unroll
-            for (int i = 0; i < Sh::kSteps; ++i) {
-                const Sh mine(lane, i, wave_u);
-                unsigned id = read_dword(lds_addr(id_ring) + ((u & (Sh::kIdDepth - 1)) * Sh::kSteps + i) * 256 + lane * 4);
-                lds_wait<0>();
-                tie(id);
-                const int t = u + !mine.is_v;
-                const long long at =
-                    t >= t0 && t < min(t_end, ntp) ? row_of(p, g, pc.real(t) * KT + mine.key, (int)id, pc.L, pc.sp) : -1;
-                const long long row = max(at, 0ll);
-                unsigned char *to = raw + (u & (Sh::kDepth - 1)) * Sh::kBytes + i * 1280;
-                __builtin_amdgcn_global_load_lds(
-                    (const GLOBAL_AS void *)((mine.is_v ? p.v4 : p.k4) + row * (D / 2) + mine.blk * 16), (LDS_AS void *)to, 16, 0, 0);
-                __builtin_amdgcn_global_load_lds(
-                    (const GLOBAL_AS void *)(p.scales + row * (D / 16) + (D == 128 && mine.is_v ? 4 : 0)),
-                    (LDS_AS void *)(to + 1024), 4, 0, 0);
+            if constexpr (!SMALL) {
+                const long long row_k = first_row(u + 1, id_k);
+                #pragma unroll
+                for (int i = 0; i < Sh::kSteps; ++i) {
+                    const Sh mine(lane, i);
+                    const uint8_t *codes = mine.is_v ? p.v4 + row_v * (D / 2) : p.k4 + row_k * (D / 2);
+                    const uint8_t *scales = p.scales + (mine.is_v ? row_v : row_k) * (D / 16);
+                    load_from(u, i, codes + (mine.key * (D / 2) + mine.blk * 16),
+                              scales + (mine.key * (D / 16) + (D == 128 && mine.is_v ? 4 : 0)));
+                }
+                row_v = row_k;
+                id_k = id_of(u + 2);
+            } else {
+                #pragma unroll
+                for (int i = 0; i < Sh::kSteps; ++i) {
+                    const Sh mine(lane, i);
+                    unsigned id = read_dword(lds_addr(id_ring) + ((u & (Sh::kIdDepth - 1)) * Sh::kSteps + i) * 256 + lane * 4);
+                    lds_wait<0>();
+                    tie(id);
+                    const int t = u + !mine.is_v, at = pc.real(t) * KT + wave_u * KPW + mine.key;
+                    const long long row =
+                        max(t >= t0 && t < tp_end ? row_of(p, g, at, (int)id, pc.L, pc.sp) : -1ll, 0ll);
+                    load_from(u, i, (mine.is_v ? p.v4 : p.k4) + row * (D / 2) + mine.blk * 16,
+                              p.scales + row * (D / 16) + (D == 128 && mine.is_v ? 4 : 0));
+                }
             }
         };
-        #pragma unroll
-        for (int i = -1; i < 3; ++i) load_ids(t0 + i);
+        if constexpr (SMALL) {
+            #pragma unroll
+            for (int i = -1; i < 3; ++i) load_ids(t0 + i);
+        } else {
+            id_k = id_of(t0);
+        }
 
         // ---- this wave's 32 query rows: a row past the unit's last one loads the unit's first
         const int row0 = pc.rb * p.rows_per_block, row_at = row0 + wave_u * kRowsPerWave + col;
@@ -176,24 +209,34 @@ __global__ __launch_bounds__(NW * kWave) void kv4_wide_kernel(Kv4AttnParams p) {
         };
         // Conversion of the share of period u. A key that no node sees counts as zeros.
         auto convert = [&](int u) {
+            const int base_k = pc.real(u + 1) * KT, base_v = pc.real(u) * KT;
+            auto clear = [&](int base) { return base + KT <= pc.L && (base >= pc.sp.lo || base + KT <= pc.sp.sinks); };
+            const bool all = clear(base_k) && clear(base_v);
             #pragma unroll
             for (int i = 0; i < Sh::kSteps; ++i) {
-                const Sh mine(lane, i, wave_u);
+                const Sh mine(lane, i);
                 const unsigned from = lds_addr(raw) + (u & (Sh::kDepth - 1)) * Sh::kBytes + i * 1280;
                 u32x4 x = read_codes(from + lane * 16);
                 unsigned sc = read_dword(from + 1024 + lane * 4);
-                const int t = u + !mine.is_v, at = pc.real(t) * KT + mine.key;
-                const bool live = at < pc.L && (at >= pc.sp.lo || at < pc.sp.sinks);
-                const unsigned to = ring + (t & 1) * Gm::kStageBytes + (mine.is_v ? Gm::kTileBytes : 0) +
-                                    mine.key * Gm::kRowBytes + (((mine.blk * 4) ^ swz<C>(mine.key % C)) << 4);
+                const int key = wave_u * KPW + mine.key;
+                // stages (u + 1) & 1 for K and u & 1 for V
+                const unsigned to = ring + ((key * Gm::kRowBytes + (((mine.blk * 4) ^ swz<C>(key % C)) << 4) +
+                                             (mine.is_v ? Gm::kTileBytes : Gm::kStageBytes)) ^
+                                            ((u & 1) * Gm::kStageBytes));
                 lds_wait<0>();
                 tie(x);
                 tie(sc);
-                const unsigned e = (sc >> (8 * (mine.blk + (D == 64 && mine.is_v ? 2 : 0)))) & 255u;
-                if (t < ntp) {
+                unsigned e = (sc >> (8 * (mine.blk + (D == 64 && mine.is_v ? 2 : 0)))) & 255u;
+                if (!all) {
+                    const int at = (mine.is_v ? base_v : base_k) + key;
+                    if (!(at < pc.L && (at >= pc.sp.lo || at < pc.sp.sinks))) {
+                        x = u32x4{0, 0, 0, 0};
+                        e = 127;
+                    }
+                }
+                if (u + !mine.is_v < ntp) {
                     #pragma unroll
-                    for (int q = 0; q < 4; ++q)
-                        write_chunk(to ^ (q << 4), from4x8(live ? x[q] : 0u, scale4(live ? e : 127u)));
+                    for (int q = 0; q < 4; ++q) write_chunk(to ^ (q << 4), from4x8(x[q], scale4(e)));
                 }
             }
         };
@@ -204,16 +247,16 @@ __global__ __launch_bounds__(NW * kWave) void kv4_wide_kernel(Kv4AttnParams p) {
             else build_ancestor_masks_wave_lds(p, b);
         }
         if (paths) anc_b = b;
-        wait_vmcnt<0>();
         // in the order of the loop below, whose waits count: codes of period u, ids of u + 2
+        if (SMALL) wait_vmcnt<0>();
         load_codes(t0 - 1);
         load_codes(t0);
-        load_ids(t0 + 3);
+        if (SMALL) load_ids(t0 + 3);
         load_codes(t0 + 1);
-        load_ids(t0 + 4);
+        if (SMALL) load_ids(t0 + 4);
         load_codes(t0 + 2);
         if (t0 < ntp) {
-            wait_vmcnt<3 * Sh::kLoads + 2 * Sh::kSteps>();
+            wait_vmcnt<3 * L4 + 2 * LID>();
             convert(t0 - 1);
         } else {
             load_tree(t0, false);
@@ -244,12 +287,14 @@ __global__ __launch_bounds__(NW * kWave) void kv4_wide_kernel(Kv4AttnParams p) {
         auto close = [&](int t) {
             // the codes of period t: behind them those of two periods, and ids
             if (t < ntp) {
-                wait_vmcnt<2 * (Sh::kLoads + Sh::kSteps)>();
+                wait_vmcnt<2 * (L4 + LID)>();
                 convert(t);
             }
-            // the ids of period t + 3: behind them one period's ids and two periods' codes
-            wait_vmcnt<2 * Sh::kLoads + Sh::kSteps>();
-            load_ids(t + 5);
+            if constexpr (SMALL) {
+                // the ids of period t + 3: behind them one period's ids and two periods' codes
+                wait_vmcnt<2 * L4 + LID>();
+                load_ids(t + 5);
+            }
             load_codes(t + 3);
         };
         open(t0);
@@ -336,10 +381,11 @@ __global__ __launch_bounds__(NW * kWave) void kv4_wide_kernel(Kv4AttnParams p) {
 
 template <int D>
 hipError_t launch_d(const Kv4AttnParams &p, hipStream_t s) {
+    auto go = [&](auto kernel, int waves) { return launch_kernel(kernel, dim3(p.num_wg), dim3(waves * kWave), s, p); };
     if (p.rows_per_block == 128)
-        return launch_kernel(kv4_wide_kernel<D, 4>, dim3(p.num_wg), dim3(4 * kWave), s, p);
+        return p.P < KT / 4 ? go(kv4_wide_kernel<D, 4, true>, 4) : go(kv4_wide_kernel<D, 4, false>, 4);
     if (p.rows_per_block == 256)
-        return launch_kernel(kv4_wide_kernel<D, 8>, dim3(p.num_wg), dim3(8 * kWave), s, p);
+        return p.P < KT / 8 ? go(kv4_wide_kernel<D, 8, true>, 8) : go(kv4_wide_kernel<D, 8, false>, 8);
     return hipErrorInvalidValue;
 }
 

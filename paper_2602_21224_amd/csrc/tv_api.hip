@@ -350,6 +350,7 @@ void window_params(tv::WindowAttnParams &p, const uint16_t *q, const uint16_t *k
 constexpr int kKv4StreamRows = 32;
 constexpr int kKv4StreamSetupTiles = 4;
 constexpr int kKv4StreamMinShareTiles = 8;
+constexpr int kKv4StreamWgPerCu = 2;
 
 AttnShape kv4_shape(int N, int Hq, int Hkv) {
     AttnShape s = attn_shape(N, Hq, Hkv);
@@ -357,6 +358,10 @@ AttnShape kv4_shape(int N, int Hq, int Hkv) {
     s.row_blocks = (s.rows + s.rows_per_block - 1) / s.rows_per_block;
     s.tree_tiles_all = s.row_blocks * ((N + tv::kKeyTile - 1) / tv::kKeyTile);      // at most
     return s;
+}
+
+int kv4_max_wg(const AttnShape &s) {
+    return cu_count() * (s.rows <= kKv4StreamRows ? kKv4StreamWgPerCu : kWgPerCu);
 }
 
 }  // namespace
@@ -715,7 +720,8 @@ int tree_verify_attention_window(const uint16_t *q, const uint16_t *k_tree, cons
 
 size_t tv_kv4_attention_workspace_size(int B, int N, int Hq, int Hkv, int D) {
     if (!attn_shape_ok(B, N, Hq, Hkv, D)) return 0;
-    return attn_workspace(kv4_shape(N, Hq, Hkv), D, cu_count() * kWgPerCu, true).total;
+    const AttnShape s = kv4_shape(N, Hq, Hkv);
+    return attn_workspace(s, D, kv4_max_wg(s), true).total;
 }
 
 int tree_verify_attention_kv4(const uint16_t *q, const uint16_t *k_tree, const uint16_t *v_tree, const uint8_t *k4,
@@ -732,7 +738,7 @@ int tree_verify_attention_kv4(const uint16_t *q, const uint16_t *k_tree, const u
         !aligned16(scales) || !aligned16(out) || !aligned16(workspace))
         return TV_ERR_ALIGN;
     const AttnShape s = kv4_shape(N, Hq, Hkv);
-    const int max_wg = cu_count() * kWgPerCu;
+    const int max_wg = kv4_max_wg(s);
     const AttnWorkspace ws = attn_workspace(s, D, max_wg, true);
     if (workspace_bytes < ws.total) return TV_ERR_WORKSPACE;
     const bool stream_waves = s.rows <= kKv4StreamRows;
