@@ -23,7 +23,9 @@
 //     converts the same part of V's row and stores it to a row-major half tile of the wave's
 //     own in LDS (16-byte chunks swizzled by the key), and ds_read_b64_tr_b16 reads it
 //     transposed, with the key order that the scores' accumulators have.
-// The codes of a wave's next tile are on their way in registers while it computes one.
+// The registers that held a tile's codes of K take the next tile's as soon as its scores are
+// under way, those of V when V is in LDS: loads are on their way for most of a tile's time, and
+// with two sets of registers (a set more in flight) a wave spilled.
 #include "tree_attention_kv4.h"
 
 namespace tv {
@@ -50,34 +52,30 @@ constexpr int kStreamWaves = 4;
 __shared__ __attribute__((aligned(1024))) unsigned char g_half[kStreamWaves * Geo<128>::kTileBytes / 2];
 __shared__ float g_ml[kStreamWaves][16][2];
 
-// Loads of the prefix tile at position `base`; a key block without a page reads the cache's
-// first rows. SMALL: pages of fewer than 16 keys, so every lane has its own.
-template <int D, bool SMALL>
-__device__ __forceinline__ void load_raw(const Kv4AttnParams &p, const Piece &pc, int base, int lane, Raw4<D> &r) {
-    const int c = lane & 15, g = lane >> 4;
+// Rows of the cache (of one KV head's tokens) that hold the key blocks of the prefix tile at
+// position `base`; a block without a page takes the cache's first rows. SMALL: pages of fewer
+// than 16 keys, so every lane has its own.
+template <bool SMALL>
+__device__ __forceinline__ void find_rows(const Kv4AttnParams &p, const Piece &pc, int base, int c, long long (&row)[4]) {
     const int32_t *pages = p.page_table + (size_t)pc.b * p.max_pages;
-    const uint8_t *kb_at[4], *vb_at[4], *sb_at[4];
     #pragma unroll
     for (int kb = 0; kb < 4; ++kb) {
         const int at = base + 16 * kb + (SMALL ? c : 0);
         const int page = min(at >> p.p_shift, p.max_pages - 1);
         const int id = SMALL ? pages[page] : ((const CONST_AS int32_t *)pages)[page];
-        long long row = (((long long)(unsigned)id * (unsigned)p.Hkv + (unsigned)pc.g) << p.p_shift) + (at & (p.P - 1));
-        if ((unsigned)id >= (unsigned)p.num_pages) row = 0;
-        kb_at[kb] = p.k4 + row * (D / 2);
-        vb_at[kb] = p.v4 + row * (D / 2);
-        sb_at[kb] = p.scales + row * (D / 16);
+        row[kb] = (((long long)(unsigned)id * (unsigned)p.Hkv + (unsigned)pc.g) << p.p_shift) + (at & (p.P - 1));
+        if ((unsigned)id >= (unsigned)p.num_pages) row[kb] = 0;
     }
-    const unsigned rows = SMALL ? 0 : c, blk = (g * (D / 4)) / kBlock4;
+}
+
+template <int D, bool SMALL>
+__device__ __forceinline__ void load_part(const Kv4AttnParams &p, const long long (&row)[4], bool is_v, int lane,
+                                          unsigned (&x)[4][D / 32], unsigned (&e)[4]) {
+    const int c = SMALL ? 0 : lane & 15, g = lane >> 4;
     #pragma unroll
     for (int kb = 0; kb < 4; ++kb) {
-        load_dwords(r.k[kb], kb_at[kb] + (rows * (D / 2) + g * (D / 8)));
-        r.ks[kb] = sb_at[kb][rows * (D / 16) + blk];
-    }
-    #pragma unroll
-    for (int kb = 0; kb < 4; ++kb) {
-        load_dwords(r.v[kb], vb_at[kb] + (rows * (D / 2) + g * (D / 8)));
-        r.vs[kb] = sb_at[kb][rows * (D / 16) + D / kBlock4 + blk];
+        load_dwords(x[kb], (is_v ? p.v4 : p.k4) + row[kb] * (D / 2) + (unsigned)(c * (D / 2) + g * (D / 8)));
+        e[kb] = (p.scales + row[kb] * (D / 16))[(unsigned)(c * (D / 16) + (is_v ? D / kBlock4 : 0) + g * (D / 4) / kBlock4)];
     }
 }
 
@@ -98,9 +96,10 @@ __device__ __forceinline__ void drop_unseen(const Piece &pc, int base, int c, Ra
 
 // One tile: kfrag(kb, t) and vfrag(kb, t) give eight values of the lane's key of block kb,
 // from head-dim index (D/4) g + 8 t on; `vis` the keys that the lane's row of tile nr sees.
-template <int D, int NR, typename K, typename V, typename Vis>
-__device__ __forceinline__ void stream_tile(StreamState<D, NR> &st, unsigned char *vhalf, K kfrag, V vfrag,
-                                            bool masked, Vis vis, float cs, int lane) {
+// k_done and v_done are called when the lane's codes of K, of V are not needed any more.
+template <int D, int NR, typename K, typename V, typename KD, typename VD, typename Vis>
+__device__ __forceinline__ void stream_tile(StreamState<D, NR> &st, unsigned char *vhalf, K kfrag, V vfrag, KD k_done,
+                                            VD v_done, bool masked, Vis vis, float cs, int lane) {
     using Gm = Geo<D>;
     constexpr int C = Gm::kChunks;
     constexpr int NKS = D / 32, NDB = D / 16;
@@ -117,46 +116,61 @@ __device__ __forceinline__ void stream_tile(StreamState<D, NR> &st, unsigned cha
             for (int nr = 0; nr < NR; ++nr)
                 s[kb][nr] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, st.qf[nr][t], s[kb][nr], 0, 0, 0);
         }
+        __builtin_amdgcn_sched_barrier(0);     // one key block's operands at a time in registers
     }
     // V of keys 32 kst .. + 31 to LDS, and its transposing reads; LDS keeps a wave's order, so
     // the second half may follow the first's reads into the same place
-    const unsigned vbase = lds_addr(vhalf);
-    u32x2 v[2][NDB][2];
+    // (chunk numbers differ in bits that the swizzle's XOR passes on, so one address each is
+    // kept, and made opaque: otherwise every chunk's is, in registers that then spill)
+    unsigned to = lds_addr(vhalf) + c * Gm::kRowBytes + (((NKS * g) ^ swz<C>(c % C)) << 4);
+    unsigned from;
+    {
+        const int key = 4 * g + (c >> 2);
+        from = lds_addr(vhalf) + key * Gm::kRowBytes + ((((c & 3) >> 1) ^ swz<C>(key % C)) << 4) + (c & 1) * 8;
+    }
+    tie(to);
+    tie(from);
+    u32x2 v[NDB][2];
     auto store_v = [&](int kst) {
         #pragma unroll
         for (int r = 0; r < 2; ++r)
             #pragma unroll
             for (int t = 0; t < NKS; ++t) {
-                const int key = 16 * r + c;
-                *reinterpret_cast<bf16x8 *>(vhalf + key * Gm::kRowBytes + (((NKS * g + t) ^ swz<C>(key % C)) << 4)) =
-                    vfrag(2 * kst + r, t);
+                const bf16x8 x = vfrag(2 * kst + r, t);
+                asm volatile("ds_write_b128 %0, %1 offset:%2"
+                             ::"v"(to ^ (t << 4)), "v"(__builtin_bit_cast(u32x4, x)), "i"(r * 16 * Gm::kRowBytes)
+                             : "memory");
             }
     };
-    auto read_v = [&](int kst) {
+    auto read_v = [&]() {
         #pragma unroll
         for (int db = 0; db < NDB; ++db)
             #pragma unroll
             for (int r = 0; r < 2; ++r) {
-                const int key = 16 * r + 4 * g + (c >> 2);
-                const int chunk = 2 * db + ((c & 3) >> 1);
-                const unsigned addr =
-                    vbase + key * Gm::kRowBytes + ((unsigned)(chunk ^ swz<C>(key % C)) << 4) + (c & 1) * 8;
-                asm volatile("ds_read_b64_tr_b16 %0, %1" : "=v"(v[kst][db][r]) : "v"(addr) : "memory");
+                // key 16 r + 4 g + (c >> 2) has the swizzle of 4 g + (c >> 2) up to a multiple of C
+                const unsigned at = from ^ ((unsigned)((2 * db) ^ swz<C>((16 * r) % C)) << 4);
+                asm volatile("ds_read_b64_tr_b16 %0, %1 offset:%2"
+                             : "=v"(v[db][r]) : "v"(at), "i"(r * 16 * Gm::kRowBytes) : "memory");
             }
     };
+    k_done();
+    __builtin_amdgcn_sched_barrier(0);
     store_v(0);
-    read_v(0);
+    read_v();
     store_v(1);
+    v_done();
+    __builtin_amdgcn_sched_barrier(0);
     bf16x8 pb[NR][2];
     #pragma unroll
     for (int nr = 0; nr < NR; ++nr) {
         if (masked) {
-            const unsigned long long x = vis(nr);
+            const unsigned long long x = vis(nr) >> (4 * g);
+            const unsigned half[2] = {(unsigned)x, (unsigned)(x >> 32)};
             #pragma unroll
             for (int kb = 0; kb < 4; ++kb)
                 #pragma unroll
                 for (int i = 0; i < 4; ++i)
-                    s[kb][nr][i] = ((x >> (kb * 16 + 4 * g + i)) & 1ull) ? s[kb][nr][i] : kNegInf;
+                    s[kb][nr][i] = (half[kb >> 1] >> ((kb & 1) * 16 + i)) & 1u ? s[kb][nr][i] : kNegInf;
         }
         float mt = kNegInf;
         #pragma unroll
@@ -189,16 +203,19 @@ __device__ __forceinline__ void stream_tile(StreamState<D, NR> &st, unsigned cha
     }
     #pragma unroll
     for (int kst = 0; kst < 2; ++kst) {
+        if (kst == 1) {
+            __builtin_amdgcn_sched_barrier(0);     // into the registers that the first half leaves
+            read_v();
+        }
         lds_wait<0>();
         #pragma unroll
         for (int db = 0; db < NDB; ++db) {
-            tie(v[kst][db][0]);
-            tie(v[kst][db][1]);
+            tie(v[db][0]);
+            tie(v[db][1]);
         }
-        if (kst == 0) read_v(1);               // in flight during the first half's products
         #pragma unroll
         for (int db = 0; db < NDB; ++db) {
-            const u32x4 a = {v[kst][db][0][0], v[kst][db][0][1], v[kst][db][1][0], v[kst][db][1][1]};
+            const u32x4 a = {v[db][0][0], v[db][0][1], v[db][1][0], v[db][1][1]};
             #pragma unroll
             for (int nr = 0; nr < NR; ++nr)
                 st.o[nr][db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), pb[nr][kst],
@@ -208,7 +225,7 @@ __device__ __forceinline__ void stream_tile(StreamState<D, NR> &st, unsigned cha
 }
 
 template <int D, int NR, bool SMALL>
-__global__ __launch_bounds__(kStreamWaves * kWave, 2) void kv4_stream_kernel(Kv4AttnParams p) {
+__global__ __launch_bounds__(kStreamWaves * kWave, NR == 4 ? 1 : 2) void kv4_stream_kernel(Kv4AttnParams p) {
     using Gm = Geo<D>;
     constexpr int NW = kStreamWaves, NT = NW * kWave;
     constexpr int R = 16 * NR;
@@ -262,39 +279,39 @@ __global__ __launch_bounds__(kStreamWaves * kWave, 2) void kv4_stream_kernel(Kv4
         // ---- this wave's tiles; behind the last one its loads are repeated
         const int tp_end = min(pc.t_end, ntp);
         auto base_of = [&](int t) { return pc.real(min(t, tp_end - 1)) * KT; };
-        auto prefix_tile = [&](int t, Raw4<D> &raw) {
-            const int base = base_of(t);
-            if (base + KT > pc.L || (base < pc.sp.lo && base + KT > pc.sp.sinks)) drop_unseen<D>(pc, base, c, raw);
-            stream_tile<D, NR>(
-                st, vhalf, [&](int kb, int i) { return from4x8(raw.k[kb][i], scale4(raw.ks[kb])); },
-                [&](int kb, int i) { return from4x8(raw.v[kb][i], scale4(raw.vs[kb])); },
-                base + KT > pc.L || !window_clear(pc.sp, base, p.N),
-                [&](int nr) { return prefix_bits(p, pc, base, node[nr]); }, p.scale_log2, lane);
-        };
         int t = pc.t0 + wave_u;
         if (t < tp_end) {
-            Raw4<D> even, odd;
-            load_raw<D, SMALL>(p, pc, base_of(t), lane, even);
-            for (;;) {
-                load_raw<D, SMALL>(p, pc, base_of(t + NW), lane, odd);
-                prefix_tile(t, even);
-                if ((t += NW) >= tp_end) break;
-                load_raw<D, SMALL>(p, pc, base_of(t + NW), lane, even);
-                prefix_tile(t, odd);
-                if ((t += NW) >= tp_end) break;
+            Raw4<D> raw;
+            long long row[4];
+            find_rows<SMALL>(p, pc, base_of(t), c, row);
+            load_part<D, SMALL>(p, row, false, lane, raw.k, raw.ks);
+            load_part<D, SMALL>(p, row, true, lane, raw.v, raw.vs);
+            for (; t < tp_end; t += NW) {
+                const int base = base_of(t);
+                find_rows<SMALL>(p, pc, base_of(t + NW), c, row);
+                if (base + KT > pc.L || (base < pc.sp.lo && base + KT > pc.sp.sinks)) drop_unseen<D>(pc, base, c, raw);
+                stream_tile<D, NR>(
+                    st, vhalf, [&](int kb, int i) { return from4x8(raw.k[kb][i], scale4(raw.ks[kb])); },
+                    [&](int kb, int i) { return from4x8(raw.v[kb][i], scale4(raw.vs[kb])); },
+                    [&]() { load_part<D, SMALL>(p, row, false, lane, raw.k, raw.ks); },
+                    [&]() { load_part<D, SMALL>(p, row, true, lane, raw.v, raw.vs); },
+                    base + KT > pc.L || !window_clear(pc.sp, base, p.N),
+                    [&](int nr) { return prefix_bits(p, pc, base, node[nr]); }, p.scale_log2, lane);
             }
         }
         for (; t < pc.t_end; t += NW) {
             // tree rows, in bf16; a slot past the sequence's nodes reads node 0's row
-            const int j0 = (t - ntp) * KT;
+            int ln = lane;
+            tie(ln);                       // addresses are made here, not kept through the loop above
+            const int j0 = (t - ntp) * KT + (ln & 15);
             auto tree_row = [&](const uint16_t *from, int kb, int i) {
-                const int j = j0 + 16 * kb + c;
+                const int j = j0 + 16 * kb;
                 return *reinterpret_cast<const bf16x8 *>(
-                    from + (((size_t)b * p.N + (j < nodes ? j : 0)) * p.Hkv + g) * D + g4 * (D / 4) + 8 * i);
+                    from + (((size_t)b * p.N + (j < nodes ? j : 0)) * p.Hkv + g) * D + (ln >> 4) * (D / 4) + 8 * i);
             };
             stream_tile<D, NR>(
                 st, vhalf, [&](int kb, int i) { return tree_row(p.k_tree, kb, i); },
-                [&](int kb, int i) { return tree_row(p.v_tree, kb, i); }, true,
+                [&](int kb, int i) { return tree_row(p.v_tree, kb, i); }, []() {}, []() {}, true,
                 [&](int nr) { return window_path(g_anc[node[nr]], t - ntp, pc.L, p); }, p.scale_log2, lane);
         }
 
@@ -303,6 +320,9 @@ __global__ __launch_bounds__(kStreamWaves * kWave, 2) void kv4_stream_kernel(Kv4
         constexpr int kCh = D / 8;
         float *ow = reinterpret_cast<float *>(g_half);                     // [NW][16][D]
         const float cs = p.scale_log2;
+        int th = tid;
+        tie(th);
+        const int oc = th & 15, og = (th >> 4) & 3;
         #pragma unroll
         for (int nr = 0; nr < NR; ++nr) {
             const int first = rb * R + 16 * nr;
@@ -311,13 +331,13 @@ __global__ __launch_bounds__(kStreamWaves * kWave, 2) void kv4_stream_kernel(Kv4
             const float lw = rows_sum(st.l_run[nr]);
             #pragma unroll
             for (int db = 0; db < NDB; ++db)
-                *reinterpret_cast<f32x4 *>(ow + (wave_u * 16 + c) * D + db * 16 + 4 * g4) = st.o[nr][db];
-            if (g4 == 0) {
-                g_ml[wave_u][c][0] = st.m_run[nr];
-                g_ml[wave_u][c][1] = lw;
+                *reinterpret_cast<f32x4 *>(ow + (wave_u * 16 + oc) * D + db * 16 + 4 * og) = st.o[nr][db];
+            if (og == 0) {
+                g_ml[wave_u][oc][0] = st.m_run[nr];
+                g_ml[wave_u][oc][1] = lw;
             }
             __syncthreads();
-            for (int task = tid; task < 16 * kCh; task += NT) {
+            for (int task = th; task < 16 * kCh; task += NT) {
                 const int r = task / kCh, ch = task % kCh;
                 if (first + r >= rows_b) continue;
                 float M = kNegInf;

@@ -348,7 +348,7 @@ void window_params(tv::WindowAttnParams &p, const uint16_t *q, const uint16_t *k
 // Attention over a cache in 4 bits: up to 32 rows per KV head wave by wave, more in blocks of
 // 128 or 256 rows.
 constexpr int kKv4StreamRows = 32;
-constexpr int kKv4StreamSetupTiles = 4;
+constexpr int kKv4StreamSetupTiles = 8;
 constexpr int kKv4StreamMinShareTiles = 8;
 constexpr int kKv4StreamWgPerCu = 2;
 
