@@ -253,8 +253,12 @@ __global__ __launch_bounds__(kStreamWaves * kWave, NR == 4 ? 1 : 2) void kv4_str
         const int b = pc.b, g = pc.g, rb = pc.rb, nodes = pc.nodes, rows_b = pc.rows_b, ntp = pc.ntp;
 
         if (needs_paths(p, pc) && anc_b != b) {
-            // (units of at most 32 rows have at most 32 nodes)
-            if (wave_u == 0) build_ancestor_masks_wave(p, lane < p.N ? p.parent[(size_t)b * p.N + lane] : -1);
+            if (wave_u == 0) {
+                if (p.N <= kWave)
+                    build_ancestor_masks_wave(p, lane < p.N ? p.parent[(size_t)b * p.N + lane] : -1);
+                else
+                    build_ancestor_masks_wave_lds(p, b);
+            }
             anc_b = b;
             __syncthreads();
         }

@@ -345,23 +345,37 @@ void window_params(tv::WindowAttnParams &p, const uint16_t *q, const uint16_t *k
     p.window = window; p.sinks = sinks;
 }
 
-// Attention over a cache in 4 bits: up to 32 rows per KV head wave by wave, more in blocks of
-// 128 or 256 rows.
-constexpr int kKv4StreamRows = 32;
+// Attention over a cache in 4 bits: few rows per KV head wave by wave, in blocks of 16 or 32
+// rows (tree_attention_kv4.hip), many in blocks of 128 or 256 by workgroups
+// (tree_attention_kv4_wide.hip). Measured (us per call, head size 128, by waves and by
+// workgroups): 64 sequences of 200-500 tokens, 64 rows 50 and 56, 68 rows 62 and 56, 96 rows 67
+// and 57 (every block takes the tree's tiles again); 16 sequences of 500-900 tokens, 96 rows 35
+// and 32; of 1024-4096 tokens, 64 rows 41 and 62, 96 rows 51 and 63, 128 rows 63 and 64, 160 rows
+// 73 and 67; 4 sequences of 32768 tokens, 128 rows 115 and 154, 160 rows 142 and 165, 192 rows
+// 162 and 166.
+// Shares: of 2, 4, 6, 8 and 12 set-up tiles per unit and 4, 6 and 8 tiles at least per share the
+// smallest calls took 17.3 to 13.3, 8 and 8 13.8, the larger ones the same within their noise.
+constexpr int kv4_stream_rows(long prefix) {
+    return prefix < 1024 ? 64 : prefix < 16384 ? 96 : 160;
+}
 constexpr int kKv4StreamSetupTiles = 8;
 constexpr int kKv4StreamMinShareTiles = 8;
 constexpr int kKv4StreamWgPerCu = 2;
 
-AttnShape kv4_shape(int N, int Hq, int Hkv) {
-    AttnShape s = attn_shape(N, Hq, Hkv);
-    s.rows_per_block = s.rows <= 16 ? 16 : s.rows <= kKv4StreamRows ? 32 : s.rows <= 128 ? 128 : 256;
+struct Kv4Shape : AttnShape {
+    bool stream;
+    int max_wg;
+};
+
+Kv4Shape kv4_shape(int N, int Hq, int Hkv, long prefix) {
+    Kv4Shape s;
+    static_cast<AttnShape &>(s) = attn_shape(N, Hq, Hkv);
+    s.stream = s.rows <= kv4_stream_rows(prefix);
+    s.max_wg = cu_count() * (s.stream ? kKv4StreamWgPerCu : kWgPerCu);
+    s.rows_per_block = s.stream ? (s.rows <= 16 ? 16 : 32) : s.rows <= 128 ? 128 : 256;
     s.row_blocks = (s.rows + s.rows_per_block - 1) / s.rows_per_block;
     s.tree_tiles_all = s.row_blocks * ((N + tv::kKeyTile - 1) / tv::kKeyTile);      // at most
     return s;
-}
-
-int kv4_max_wg(const AttnShape &s) {
-    return cu_count() * (s.rows <= kKv4StreamRows ? kKv4StreamWgPerCu : kWgPerCu);
 }
 
 }  // namespace
@@ -720,8 +734,13 @@ int tree_verify_attention_window(const uint16_t *q, const uint16_t *k_tree, cons
 
 size_t tv_kv4_attention_workspace_size(int B, int N, int Hq, int Hkv, int D) {
     if (!attn_shape_ok(B, N, Hq, Hkv, D)) return 0;
-    const AttnShape s = kv4_shape(N, Hq, Hkv);
-    return attn_workspace(s, D, kv4_max_wg(s), true).total;
+    size_t need = 0;
+    for (long prefix : {0L, (long)INT_MAX}) {       // the most rows to either kernel
+        const Kv4Shape s = kv4_shape(N, Hq, Hkv, prefix);
+        const size_t n = attn_workspace(s, D, s.max_wg, true).total;
+        if (need < n) need = n;
+    }
+    return need;
 }
 
 int tree_verify_attention_kv4(const uint16_t *q, const uint16_t *k_tree, const uint16_t *v_tree, const uint8_t *k4,
@@ -737,16 +756,15 @@ int tree_verify_attention_kv4(const uint16_t *q, const uint16_t *k_tree, const u
     if (!aligned16(q) || !aligned16(k_tree) || !aligned16(v_tree) || !aligned16(k4) || !aligned16(v4) ||
         !aligned16(scales) || !aligned16(out) || !aligned16(workspace))
         return TV_ERR_ALIGN;
-    const AttnShape s = kv4_shape(N, Hq, Hkv);
-    const int max_wg = kv4_max_wg(s);
-    const AttnWorkspace ws = attn_workspace(s, D, max_wg, true);
-    if (workspace_bytes < ws.total) return TV_ERR_WORKSPACE;
-    const bool stream_waves = s.rows <= kKv4StreamRows;
-    const int setup = stream_waves ? kKv4StreamSetupTiles : kSetupTiles;
-    auto tiles_of = [&](long tiles) {
-        return (long)B * Hkv * ((long)s.row_blocks * (tiles + setup) + s.tree_tiles_all);
-    };
+    if (workspace_bytes < tv_kv4_attention_workspace_size(B, N, Hq, Hkv, D)) return TV_ERR_WORKSPACE;
     const long max_len = (long)max_pages * P;
+    const long tiles = window_tiles(max_kv_len < max_len ? max_kv_len : max_len, window, sinks);
+    const Kv4Shape s = kv4_shape(N, Hq, Hkv, tiles * tv::kKeyTile);
+    const AttnWorkspace ws = attn_workspace(s, D, s.max_wg, true);
+    const int setup = s.stream ? kKv4StreamSetupTiles : kSetupTiles;
+    auto tiles_of = [&](long prefix) {
+        return (long)B * Hkv * ((long)s.row_blocks * (prefix + setup) + s.tree_tiles_all);
+    };
     if (tiles_of((max_len + tv::kKeyTile - 1) / tv::kKeyTile) >= kMaxTiles) return TV_ERR_SHAPE;
     if (!device_ok()) return TV_ERR_DEVICE;
 
@@ -755,10 +773,9 @@ int tree_verify_attention_kv4(const uint16_t *q, const uint16_t *k_tree, const u
                   window, sinks, scale, out, lse, workspace, ws);
     p.k4 = k4; p.v4 = v4; p.scales = scales;
     p.g_inv = s.G == 1 ? 0u : (unsigned)((1ull << 32) / (unsigned)s.G + 1);
-    long num_wg = tiles_of(window_tiles(max_kv_len < max_len ? max_kv_len : max_len, window, sinks)) /
-                  (stream_waves ? kKv4StreamMinShareTiles : kMinShareTiles);
+    long num_wg = tiles_of(tiles) / (s.stream ? kKv4StreamMinShareTiles : kMinShareTiles);
     if (num_wg < 1) num_wg = 1;
-    if (num_wg > max_wg) num_wg = max_wg;
+    if (num_wg > s.max_wg) num_wg = s.max_wg;
     p.rows_per_block = s.rows_per_block;
     p.setup_tiles = setup;
     p.num_wg = (int)num_wg;

@@ -26,6 +26,12 @@ CASES = [
     (2, 100, 12, 2, 128, 64, [640, 0], 0, 0, "chain", True),      # 600 rows
     (1, 256, 8, 1, 64, 256, [700], 0, 0, "capped", False),        # 2048 rows, long pages
     (1, 256, 2, 1, 128, 32, [190], 0, 0, "chain", False),         # the deepest tree
+    (2, 50, 4, 2, 128, 16, [200, 900], 0, 0, "forest", True),     # 100 rows
+    (2, 110, 1, 1, 64, 32, [333, 64], 0, 0, "capped", True),      # 110 rows, a tree of two tiles
+    (2, 41, 6, 2, 128, 4, [250, 70], 0, 0, "forest", False),      # 123 rows, pages of 4
+    (3, 25, 2, 1, 64, 2, [250, 0, 64], 0, 0, "capped", False),    # 50 rows, pages of 2
+    (1, 90, 1, 1, 128, 8, [129], 0, 0, "chain", False),           # 90 rows, a tree of two tiles
+    (2, 70, 6, 3, 64, 4, [500, 191], 0, 0, "forest", True),       # 140 rows, pages of 4
     # inside a window
     (1, 1, 8, 8, 64, 16, [128], 1, 0, "chain", False),            # a token sees itself
     (3, 1, 8, 2, 128, 16, [700, 64, 5], 1, 3, "chain", False),
@@ -43,6 +49,11 @@ CASES = [
     (1, 200, 4, 2, 64, 256, [1500], 90, 300, "chain", False),     # far edges within the tree, several words
     (1, 256, 8, 1, 128, 16, [700], 650, 9, "capped", False),
     (2, 3, 16, 2, 128, 1, [5000, 2500], 1200, 70, "chain", False),    # one-token pages, several page windows
+    (2, 50, 4, 2, 64, 16, [700, 900], 300, 20, "chain", True),    # 100 rows
+    (2, 41, 6, 2, 128, 1, [250, 370], 100, 3, "forest", False),   # 123 rows, one-token pages
+    (1, 90, 1, 1, 128, 2, [429], 60, 100, "chain", False),        # 90 rows, a window shorter than the tree
+    (1, 40, 4, 1, 64, 256, [17000], 0, 0, "capped", False),       # 160 rows over a long prefix
+    (1, 48, 2, 1, 128, 16, [17000], 16900, 0, "capped", False),   # 96 rows
     (1, 1, 2, 1, 64, 1, [20000], 0, 0, "chain", False),           # one unit over all workgroups
     (1, 1, 2, 1, 128, 1, [20000], 9000, 700, "chain", False),
 ]
