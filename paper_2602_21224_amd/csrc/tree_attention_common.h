@@ -231,6 +231,13 @@ __device__ __forceinline__ float part_scale(float top, float &unscale) {
     return __builtin_amdgcn_ldexpf(1.f, 15 - e);
 }
 
+// A part's maximum in powers of two, for the joining kernel: -inf for a part that saw nothing.
+// Scores that are NaN leave the maximum alone, so that of a part of nothing else is -inf too;
+// its sum, which is NaN, stands in for it.
+__device__ __forceinline__ float part_max(float m, float l, float c) {
+    return l != l ? l : m == kNegInf ? kNegInf : m * c;
+}
+
 // Exclusive prefix sum of per-sequence tile counts into g_cum[0..B], the
 // clamped prefix lengths into g_len[0..B) and the node counts into g_nn:
 // wave 0 reads kv_len (and num_nodes) once per lane and scans with cross-lane

@@ -351,9 +351,8 @@ __global__ __launch_bounds__(kStreamWaves * kWave, NR == 4 ? 1 : 2) void kv4_str
                 float acc[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
                 #pragma unroll
                 for (int u = 0; u < NW; ++u) {
-                    const float mu = g_ml[u][r][0];
-                    if (mu == kNegInf) continue;                   // the wave saw nothing
-                    const float sc = __builtin_amdgcn_exp2f((mu - M) * cs);
+                    const float mu = g_ml[u][r][0];                // -inf: the wave saw nothing, or NaN only
+                    const float sc = mu == kNegInf ? 0.f : __builtin_amdgcn_exp2f((mu - M) * cs);
                     lsum += sc * g_ml[u][r][1];
                     const f32x4 a0 = *reinterpret_cast<const f32x4 *>(ow + (u * 16 + r) * D + ch * 8);
                     const f32x4 a1 = *reinterpret_cast<const f32x4 *>(ow + (u * 16 + r) * D + ch * 8 + 4);
@@ -374,8 +373,8 @@ __global__ __launch_bounds__(kStreamWaves * kWave, NR == 4 ? 1 : 2) void kv4_str
                         p.lse[((size_t)b * p.N + nd) * p.Hq + h] = M * p.scale + __builtin_amdgcn_logf(lsum) * kLn2;
                 } else {
                     // a piece: normalised by its own sum, fp16 times a power of two (a piece may
-                    // hold no key that the row sees: max -inf, left out by the joining kernel)
-                    const bool none = M == kNegInf;
+                    // hold no key that the row sees, and is left out by the joining kernel then)
+                    const bool none = lsum == 0.f;
                     const float top = row_top(
                         [&](auto take) {
                             #pragma unroll
@@ -395,7 +394,7 @@ __global__ __launch_bounds__(kStreamWaves * kWave, NR == 4 ? 1 : 2) void kv4_str
                     *reinterpret_cast<f16x8 *>(p.ws_o + at * D + ch * 8) = f;
                     if (ch == 0)
                         *reinterpret_cast<f32x4 *>(p.ws_ml + at * 4) =
-                            f32x4{none ? kNegInf : M * cs, none ? 0.f : lsum, none ? 1.f : unscale, 0.f};
+                            f32x4{part_max(M, lsum, cs), lsum, none ? 1.f : unscale, 0.f};
                 }
             }
         }

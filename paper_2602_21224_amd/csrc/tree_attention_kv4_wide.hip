@@ -19,9 +19,12 @@
 // The tree's rows are bf16 already and come straight into the converted tiles' places, a
 // period ahead.
 //
-// Four waves of 64 rows each, which halve the operand reads from LDS, took 88 us where this
-// takes 57 and 10 us for the merge (16 x 64 nodes x 4 heads over 1024-4096 tokens): one wave per SIMD issues an
-// instruction every 6.8 cycles, and its vector work was as long as the period.
+// Measured (16 x 64 nodes, 4 heads per KV head, over 1024-4096 tokens): 66-73 us, 10 of them
+// for joining the split rows; 640 TFLOP/s of 1310. A tile costs a CU 5100 cycles, of which the
+// matrix cores take 2048, the softmax, masks and conversions 3000 and LDS 2450, and a launch
+// has 31000 cycles beside its tiles. Four waves of 64 rows each, which halve the operand reads
+// from LDS, took 88 us: one wave per SIMD issues an instruction every 6.8 cycles, and its vector
+// work was as long as the period. Blocks of 64 rows whose waves each convert tiles of their own: 299.
 #include "tree_attention_kv4.h"
 
 namespace tv {
@@ -367,7 +370,7 @@ __global__ __launch_bounds__(NW * kWave) void kv4_wide_kernel(Kv4AttnParams p) {
                 const int rl = wave_u * kRowsPerWave + ln;
                 if (!pc.complete)
                     *reinterpret_cast<f32x4 *>(p.ws_ml + ((size_t)pc.slot * p.rows_per_block + rl) * 4) =
-                        f32x4{st.m_run == kNegInf ? kNegInf : st.m_run * p.scale_log2, l_tot, unscale, 0.f};
+                        f32x4{part_max(st.m_run, l_tot, p.scale_log2), l_tot, unscale, 0.f};
                 else if (p.lse && pc.rb * p.rows_per_block + rl < pc.rows_b)
                     p.lse[((size_t)b * p.N + node) * p.Hq + hq] =
                         st.m_run * p.scale + __builtin_amdgcn_logf(l_tot) * kLn2;

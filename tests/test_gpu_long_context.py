@@ -182,6 +182,30 @@ def test_a_block_of_nan_reaches_the_rows_that_see_it():
     assert torch.isnan(lse[0, :, :4]).all() and torch.isfinite(lse[0, :, 4:]).all() and torch.isfinite(lse[1]).all()
 
 
+@pytest.mark.parametrize("cached", ["bf16", "4 bits"])
+@pytest.mark.parametrize("B,N", [(1, 1), (1, 64), (700, 1), (300, 9), (200, 64)])
+def test_whole_tiles_of_nan_reach_the_rows_that_see_them(cached, B, N):
+    """Sequence 0's keys 64 .. 319 of KV head 0: parts of its row see nothing else."""
+    T = U.require_gpu()
+    w = LU.workload(36, B=B, N=N, Hq=8, Hkv=2, D=64, P=16, lens=[1500] + [70] * (B - 1), tree="forest")
+    d = U.upload(w)
+    cache = [U.dev(a) for a in LU.cache4(w)] if cached == "4 bits" else [d["k_cache"], d["v_cache"]]
+    f = T.tree_verify_attention_kv4 if cached == "4 bits" else T.tree_verify_attention_window
+    run = lambda: f(d["q"], d["k_tree"], d["v_tree"], *cache, d["page_table"], d["kv_len"], d["parent"],  # noqa: E731
+                    max_kv_len=1500, window=0)
+    out, lse = run()
+    assert torch.isfinite(out).all() and torch.isfinite(lse).all()
+    pages = d["page_table"][0, 4:20].long()
+    if cached == "4 bits":
+        cache[2][pages, 0, :, 0] = 255
+    else:
+        cache[0][pages, :, 0] = float("nan")
+    bad, z = run()
+    assert torch.isnan(bad[0, :, :4]).all() and torch.isnan(z[0, :, :4]).all()
+    assert same(bad[0, :, 4:], out[0, :, 4:]) and same(bad[1:], out[1:])
+    assert torch.equal(z[0, :, 4:], lse[0, :, 4:]) and torch.equal(z[1:], lse[1:])
+
+
 def test_every_scale_byte_and_code():
     """Keys of one block per scale byte; a single key is visible, so out is its values."""
     T = U.require_gpu()
