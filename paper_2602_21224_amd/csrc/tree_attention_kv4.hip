@@ -23,6 +23,15 @@
 //     converts the same part of V's row and stores it to a row-major half tile of the wave's
 //     own in LDS (16-byte chunks swizzled by the key), and ds_read_b64_tr_b16 reads it
 //     transposed, with the key order that the scores' accumulators have.
+// Bound by the stream of codes where prefixes are long: 64 sequences of 2048-8192 tokens, one
+// node x 4 heads per KV head, 79-82 us, 363 MB read at 4.5 TB/s; 4 x 4 nodes over 98304-131072
+// tokens 107 us, 4.7 TB/s (a copy reaches 4.8). 16 x 12 nodes x 32 heads over 256-2048 tokens,
+// about one unit per workgroup, take 34 us where the bytes take 18, one sequence of 2048 tokens
+// 14: the way to the first tile (lengths, search, page ids) 2.4 us, two tiles 3, the waves'
+// meeting 1.8, the launch, the joining kernel 4.
+// With four waves per CU (one workgroup, a set of registers more in flight) these were 98, 111,
+// 50 and 19; loading the first codes before the root paths are found, and the tree's tiles first,
+// 90 instead of 80 and 36 instead of 33.
 // The registers that held a tile's codes of K take the next tile's as soon as its scores are
 // under way, those of V when V is in LDS: loads are on their way for most of a tile's time, and
 // with two sets of registers (a set more in flight) a wave spilled.
@@ -49,6 +58,7 @@ struct StreamState {
 };
 
 constexpr int kStreamWaves = 4;
+constexpr int kStreamWgPerCu = 2;
 __shared__ __attribute__((aligned(1024))) unsigned char g_half[kStreamWaves * Geo<128>::kTileBytes / 2];
 __shared__ float g_ml[kStreamWaves][16][2];
 
@@ -225,7 +235,7 @@ __device__ __forceinline__ void stream_tile(StreamState<D, NR> &st, unsigned cha
 }
 
 template <int D, int NR, bool SMALL>
-__global__ __launch_bounds__(kStreamWaves * kWave, NR == 4 ? 1 : 2) void kv4_stream_kernel(Kv4AttnParams p) {
+__global__ __launch_bounds__(kStreamWaves * kWave, kStreamWgPerCu) void kv4_stream_kernel(Kv4AttnParams p) {
     using Gm = Geo<D>;
     constexpr int NW = kStreamWaves, NT = NW * kWave;
     constexpr int R = 16 * NR;

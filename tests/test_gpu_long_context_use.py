@@ -219,3 +219,66 @@ def test_rows_of_other_sequences_and_pages_stay():
     T.kv4_write(U.dev_bf16(k), U.dev_bf16(v), *dc, U.dev(table), U.dev(start), count=U.dev(count))
     want = O.write4(k, v, *cache, table, start, count=count)
     assert all(np.array_equal(a.cpu().numpy(), b) for a, b in zip(dc, want))
+
+
+@pytest.mark.parametrize("Hq,Hkv,N,D,lens", [
+    (71, 1, 1, 128, [300, 5]),                   # one KV head, 71 rows
+    (142, 2, 1, 64, [1300, 2000]),               # 71 rows, longer prefixes
+    (13, 13, 1, 64, [100, 65]),                  # a row per KV head, an odd number of heads
+    (21, 3, 5, 128, [77, 640]),                  # 35 rows
+    (45, 5, 17, 64, [130, 700]),                 # 153 rows
+    (2048, 1, 1, 64, [70, 3]),                   # the most rows by heads
+    (1000, 2, 4, 128, [70, 300]),                # 2000 rows, blocks that end within a node
+])
+@pytest.mark.parametrize("which", ["window", "4 bits"])
+def test_head_layouts(which, Hq, Hkv, N, D, lens):
+    T = U.require_gpu()
+    w, d, cache, bits, kw = setup(which, 86, 50, 4, B=2, N=N, Hq=Hq, Hkv=Hkv, D=D, lens=lens, tree="forest")
+    print(f"{which} Hq={Hq} Hkv={Hkv} N={N} D={D}", flush=True)
+    out, lse = call(T, which, d, cache, w.max_kv_len, **kw)
+    LU.check(w, U.bf16_to_f64(out), lse.cpu().numpy().astype(np.float64), LU.expected(w, 50, 4, bits), which)
+
+
+def test_refusals():
+    """Shapes, types, strides and devices that do not fit the call's other tensors."""
+    T = U.require_gpu()
+    w, d, cache, _, _ = setup("4 bits", 87)
+    wd, dd, wcache, _, _ = setup("window", 87)
+
+    def refused(match, which="4 bits", c=None, hint=900, **kw):
+        args = dict(d if which == "4 bits" else dd)
+        args.update({k: kw.pop(k) for k in list(kw) if k in args})
+        with pytest.raises((ValueError, TypeError, RuntimeError), match=match):
+            call(T, which, args, c or (cache if which == "4 bits" else wcache), hint, window=5, **kw)
+    k4, v4, sc = cache
+    refused("k4", c=[k4[..., :32], v4, sc])
+    refused("v4", c=[k4, v4[:-1], sc])
+    refused("scales", c=[k4, v4, sc[..., :2].contiguous()])
+    refused("scales", c=[k4, v4, sc.to(torch.int32)])
+    refused("k4", c=[k4.transpose(1, 2), v4, sc])            # the bf16 cache's order of heads and tokens
+    refused("v_cache", "window", c=[wcache[0], wcache[1][:, ::2]])
+    for which in ("window", "4 bits"):
+        refused("q", which, q=d["q"].float())
+        refused("k_tree", which, k_tree=d["k_tree"].cpu())
+        refused("page_table", which, page_table=d["page_table"].long())
+        refused("parent", which, parent=d["parent"][:, :-1])
+        refused("kv_len", which, kv_len=d["kv_len"][:-1])
+        refused("out", which, out=torch.empty_like(d["q"])[..., ::2])
+        refused("lse", which, lse=torch.empty(d["q"].shape[:3], dtype=torch.bfloat16, device="cuda"))
+        refused("workspace|WORKSPACE", which, workspace=torch.empty(64, dtype=torch.uint8, device="cuda"))
+        refused(".", which, hint=-1)
+        refused(".", which, sinks=-1)
+    k = torch.zeros((3, 4, 2, 128), dtype=torch.bfloat16, device="cuda")
+    start = torch.zeros(3, dtype=torch.int32, device="cuda")
+
+    def no_write(match, k=k, v=k, start=start, **kw):
+        with pytest.raises((ValueError, TypeError, RuntimeError), match=match):
+            T.kv4_write(k, v, *cache, d["page_table"], start, **kw)
+    no_write("v", v=k[:, :3])
+    no_write("k4", k=k[..., :64].contiguous(), v=k[..., :64].contiguous())
+    no_write("start", start=start.long())
+    no_write("idx", idx=torch.zeros((3, 3), dtype=torch.int32, device="cuda"))
+    no_write("count", count=torch.zeros(2, dtype=torch.int32, device="cuda"))
+    no_write("k_held", k_held=k[:, :2])
+    no_write("overlap|OVERLAP", k_held=k, idx=torch.zeros((3, 4), dtype=torch.int32, device="cuda"))
+    assert all(torch.equal(a, U.dev(b)) for a, b in zip(cache, LU.cache4(w)))
