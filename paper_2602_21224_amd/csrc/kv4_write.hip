@@ -5,8 +5,8 @@
 //                             2^-e is a normal number, and 6 2^e a bf16)
 //   code(v) = the nearest of 0, 0.5, 1, 1.5, 2, 3, 4, 6 to |v| / 2^e (ties to the even
 //             code, what exceeds 6 to 6), with v's sign
-// so the largest value is off by at most a sixth, and never cut by more than 1 2^e: with
-// x - 2 throughout, values between 7 2^e and 8 2^e would be cut to 6 2^e.
+// so the block's largest value is off by at most a fifth: with x - 2 throughout, one of nearly
+// 8 2^e would be cut to 6 2^e, a quarter off.
 //
 // A workgroup takes one KV head of as many consecutive tokens as 256 threads hold (16 at
 // head size 128): eight values per thread, so a block is a quad of lanes and its maximum two

@@ -147,18 +147,20 @@ __device__ __forceinline__ int tiles_of_sequence(int L, int nodes, const WindowA
     return p.Hkv * tiles_per_head((L + KT - 1) / KT - span_of(L, p).gap, nodes * p.G, p);
 }
 
-// Keys of the prefix tile at position `base` that a node d steps below its root sees.
-__device__ __forceinline__ unsigned long long window_bits(const Span &sp, int base, int d) {
+// Steps from node i to its root (the ancestor sets are reflexive).
+__device__ __forceinline__ int depth_of(const unsigned long long (&anc)[4]) {
+    return __popcll(anc[0]) + __popcll(anc[1]) + __popcll(anc[2]) + __popcll(anc[3]) - 1;
+}
+// Keys of the prefix tile at position `base` that the node with ancestor set `anc` sees. A piece
+// whose tiles end before the window has no ancestor sets: for it, only the sinks count.
+__device__ __forceinline__ unsigned long long window_bits(const Span &sp, int base, const unsigned long long (&anc)[4]) {
+    const int d = base + KT > sp.lo0 ? depth_of(anc) : 0;
     const int from = min(max(sp.lo0 + d - base, 0), KT), to = min(max(sp.sinks - base, 0), KT);
     return (from < KT ? ~0ull << from : 0ull) | (to < KT ? (1ull << to) - 1ull : ~0ull);
 }
 // Whether every node of a sequence of at most N sees all of that tile.
 __device__ __forceinline__ bool window_clear(const Span &sp, int base, int N) {
     return base >= sp.lo0 + N - 1 || base + KT <= sp.sinks;
-}
-// Steps from node i to its root (the ancestor sets are reflexive).
-__device__ __forceinline__ int depth_of(const unsigned long long (&anc)[4]) {
-    return __popcll(anc[0]) + __popcll(anc[1]) + __popcll(anc[2]) + __popcll(anc[3]) - 1;
 }
 // Word w of a node's root path as far as the window shows it: an ancestor's place among the
 // path's nodes is its depth, and its position L + depth.

@@ -302,7 +302,7 @@ __global__ __launch_bounds__(NW * kWave) void tree_attention_kernel(
                     vis = lim_t >= KT ? ~0ull : ((1ull << lim_t) - 1ull);
                     if (WIN && !window_clear(sp, base, p.N)) {
                         mk.masked = true;
-                        vis &= window_bits(sp, base, depth_of(g_anc[NARROW ? nnode : node]));
+                        vis &= window_bits(sp, base, g_anc[NARROW ? nnode : node]);
                     }
                 } else {
                     mk.masked = true;

@@ -135,7 +135,7 @@ __device__ __forceinline__ void load_dwords(unsigned (&to)[N], const uint8_t *fr
 __device__ __forceinline__ unsigned long long prefix_bits(const Kv4AttnParams &p, const Piece &pc, int base, int node) {
     const int lim = pc.L - base;
     unsigned long long x = lim >= KT ? ~0ull : (1ull << lim) - 1ull;
-    if (!window_clear(pc.sp, base, p.N)) x &= window_bits(pc.sp, base, depth_of(g_anc[node]));
+    if (!window_clear(pc.sp, base, p.N)) x &= window_bits(pc.sp, base, g_anc[node]);
     return x;
 }
 

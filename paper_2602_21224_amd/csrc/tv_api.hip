@@ -2,6 +2,7 @@
 // workspace carving. Every check runs on the host before any launch, so an
 // error return means nothing was enqueued.
 #include <hip/hip_runtime.h>
+#include <limits.h>
 #include <stdint.h>
 #include <string.h>
 

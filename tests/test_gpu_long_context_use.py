@@ -282,3 +282,19 @@ def test_refusals():
     no_write("k_held", k_held=k[:, :2])
     no_write("overlap|OVERLAP", k_held=k, idx=torch.zeros((3, 4), dtype=torch.int32, device="cuda"))
     assert all(torch.equal(a, U.dev(b)) for a, b in zip(cache, LU.cache4(w)))
+
+
+@pytest.mark.parametrize("N,Hq,Hkv,D", [(1, 8, 2, 128), (1, 1, 1, 64), (1, 32, 8, 128), (3, 40, 1, 128), (64, 8, 2, 64)])
+@pytest.mark.parametrize("which", ["window", "4 bits"])
+def test_a_window_that_begins_at_the_tile_behind_the_sinks(which, N, Hq, Hkv, D):
+    """The last key before the window is the last one of the sinks' tile: no node sees it, also
+    in a piece of work that has no tile of the tree, whose root paths are not looked up."""
+    T = U.require_gpu()
+    for window, sinks, n in ((4096, 4, 63), (1000, 1, 63), (2000, 65, 127), (2000, 65, 128), (640, 4, 62)):
+        w, d, cache, bits, kw = setup(which, 88 + n, window, sinks, B=1, N=N, Hq=Hq, Hkv=Hkv, D=D, lens=[window + n],
+                                      tree="chain")
+        print(f"{which} N={N} window={window} sinks={sinks} len={window + n}", flush=True)
+        zero = torch.zeros(1 << 22, device="cuda")
+        zero.sort()                              # leaves zeros in many places of LDS
+        out, lse = call(T, which, d, cache, w.max_kv_len, **kw)
+        LU.check(w, U.bf16_to_f64(out), lse.cpu().numpy().astype(np.float64), LU.expected(w, window, sinks, bits), which)
