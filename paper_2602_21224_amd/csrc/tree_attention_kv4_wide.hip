@@ -19,12 +19,14 @@
 // The tree's rows are bf16 already and come straight into the converted tiles' places, a
 // period ahead.
 //
-// Measured (16 x 64 nodes, 4 heads per KV head, over 1024-4096 tokens): 66-73 us, 10 of them
-// for joining the split rows; 640 TFLOP/s of 1310. A tile costs a CU 5100 cycles, of which the
-// matrix cores take 2048, the softmax, masks and conversions 3000 and LDS 2450, and a launch
-// has 31000 cycles beside its tiles. Four waves of 64 rows each, which halve the operand reads
-// from LDS, took 88 us: one wave per SIMD issues an instruction every 6.8 cycles, and its vector
-// work was as long as the period. Blocks of 64 rows whose waves each convert tiles of their own: 299.
+// Measured (16 x 64 nodes, 4 heads per KV head, over 1024-4096 tokens): 64-70 us, 10 of them
+// for joining the split rows. A tile costs a CU about 5000 cycles, of which the matrix cores
+// take 2048, the softmax, masks and conversions 3000 and LDS 2450; 22000 of 133000 cycles are
+// outside the tiles. Waves in their products go before those that convert (s_setprio): 4 x 64
+// nodes over 32768 tokens 167 -> 160 us, 4 x 256 nodes 600 -> 573 (over bf16: 568). Four waves of
+// 64 rows each, which halve the operand reads from LDS, took 88 us where this took 66: one wave
+// per SIMD issues an instruction every 6.8 cycles, and its vector work was as long as the period.
+// Blocks of 64 rows whose waves each convert tiles of their own: 299.
 #include "tree_attention_kv4.h"
 
 namespace tv {
@@ -305,7 +307,9 @@ __global__ __launch_bounds__(NW * kWave) void kv4_wide_kernel(Kv4AttnParams p) {
         close(t0);
         for (int t = t0 + 1; t < t_end; ++t) {
             open(t);
+            __builtin_amdgcn_s_setprio(1);         // products before the other waves' conversions
             tile_period<D, true, true>(st, s0, s1, kaddr(t), vaddr(t - 1), mk, p.scale_log2);
+            __builtin_amdgcn_s_setprio(0);
             close(t);
         }
         open(t_end);
