@@ -88,6 +88,12 @@ __device__ __forceinline__ unsigned lds_addr(const void *p) {
     return (unsigned)(size_t)(const LDS_AS void *)p;
 }
 
+// First tile with a key past the kPageCache pages from page `first` on. (Its position may
+// lie past 2^31, behind the longest prefixes.)
+__host__ __device__ __forceinline__ int page_window_end(int first, int p_shift) {
+    return (int)((((unsigned)first + kPageCache) << p_shift) / KT);
+}
+
 __device__ __forceinline__ int clamp_len(int L, const AttnParams &p) {
     const int cap = p.max_pages << p.p_shift;
     return L < 0 ? 0 : (L > cap ? cap : L);

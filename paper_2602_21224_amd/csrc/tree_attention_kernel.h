@@ -193,7 +193,7 @@ __global__ __launch_bounds__(NW * kWave) void tree_attention_kernel(
             int tb = t_end;
             if (ta < ntp) {
                 // first tile not covered
-                const int t_cov = ((page_first + kPageCache) << p.p_shift) / KT - (WIN && ta >= sp.ns ? sp.gap : 0);
+                const int t_cov = page_window_end(page_first, p.p_shift) - (WIN && ta >= sp.ns ? sp.gap : 0);
                 if (t_cov < ntp) tb = min(tb, t_cov);
                 if (WIN && SMALL && ta < sp.ns && sp.gap > 0) tb = min(tb, sp.ns);
             }

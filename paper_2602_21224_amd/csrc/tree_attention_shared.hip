@@ -380,7 +380,7 @@ __global__ __launch_bounds__(NT) void shared_attention_kernel(SharedAttnParams p
             const int page_first = (ta * KT) >> p.p_shift;
             int tb = t_end;
             if (ta < ntp) {
-                const int t_cov = ((page_first + kPageCache) << p.p_shift) / KT;   // first tile not covered
+                const int t_cov = page_window_end(page_first, p.p_shift);     // first tile not covered
                 if (t_cov < ntp) tb = min(tb, t_cov);
             }
             if (SMALL && ta < ntp) load_pages<NT>(p, b, page_first, npages);

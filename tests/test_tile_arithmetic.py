@@ -1,0 +1,49 @@
+"""The attention kernels' arithmetic on tiles and positions, compiled for the host from
+their own headers (CPU only)."""
+import ctypes
+import os
+import subprocess
+
+import pytest
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+CSRC = os.path.join(ROOT, "paper_2602_21224_amd", "csrc")
+KEYS, CACHED = 64, 512                 # keys per tile, page ids per window
+LONGEST = 0x7FFFFFFF - 1024            # tokens of the longest prefix
+
+SOURCE = """
+#include "tree_attention_common.h"
+#define API extern "C" __attribute__((visibility("default")))
+API int page_window_end(int first, int p_shift) { return tv::page_window_end(first, p_shift); }
+"""
+
+
+@pytest.fixture(scope="module")
+def host(tmp_path_factory):
+    from paper_2602_21224_amd import build
+    if not os.path.exists(build.HIPCC):
+        pytest.skip("hipcc not available")
+    d = tmp_path_factory.mktemp("tiles")
+    src, out = d / "tiles.hip", d / "libtiles.so"
+    src.write_text(SOURCE)
+    flags = [f for f in build.FLAGS if f != "-O3"]
+    subprocess.run([build.HIPCC, *flags, "-O1", "--offload-host-only", "-I", CSRC, "-shared", str(src), "-o",
+                    str(out)], check=True, capture_output=True)
+    return ctypes.CDLL(str(out))
+
+
+@pytest.mark.parametrize("shift", range(9))
+@pytest.mark.parametrize("back", [1, 64, 100000, 131072, 200000])
+def test_sub_ranges_of_a_piece_reach_its_end(host, shift, back):
+    """A piece's tiles are taken in sub-ranges whose pages fit the table of page ids: each
+    begins where the last one ended and takes whole tiles, up to the longest prefix."""
+    P = 1 << shift
+    L = LONGEST // P * P
+    tiles = -(-L // KEYS)
+    for t0 in (max(tiles - 1 - back // KEYS, 0), tiles - 1):
+        t = t0
+        while t < tiles:
+            first = t * KEYS >> shift
+            end = host.page_window_end(first, shift)
+            assert end == (first + CACHED) * P // KEYS and end > t
+            t = min(end, tiles)
