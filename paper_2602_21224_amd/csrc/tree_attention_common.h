@@ -94,8 +94,9 @@ __host__ __device__ __forceinline__ int page_window_end(int first, int p_shift) 
     return (int)((((unsigned)first + kPageCache) << p_shift) / KT);
 }
 
-__device__ __forceinline__ int clamp_len(int L, const AttnParams &p) {
-    const int cap = p.max_pages << p.p_shift;
+__host__ __device__ __forceinline__ int clamp_len(int L, const AttnParams &p) {
+    const long room = (long)p.max_pages << p.p_shift;
+    const int cap = room < kMaxPrefix ? (int)room : kMaxPrefix;
     return L < 0 ? 0 : (L > cap ? cap : L);
 }
 

@@ -316,8 +316,7 @@ bool window_shape_ok(int B, int N, int Hq, int Hkv, int D, int P, int max_pages,
                      int window, int sinks) {
     return attn_shape_ok(B, N, Hq, Hkv, D) && pow2(P) && P <= 256 && max_pages >= 1 && num_pages >= 1 &&
            max_kv_len >= 0 && window >= 0 && sinks >= 0 &&
-           // positions, those of the nodes too, are ints
-           (long)max_pages * P <= 0x7FFFFFFFl - 4 * tv::kMaxNodes;
+           (long)max_pages * P <= tv::kMaxPrefix;
 }
 
 long window_tiles(long len, int window, int sinks) {

@@ -25,6 +25,7 @@ constexpr int kNumXcd = 8;           // MI355X: 8 XCDs, workgroups dispatched ro
 constexpr int kKeyTile = 64;         // keys per attention tile (two 32-key MFMA blocks)
 constexpr int kRowsPerWave = 32;     // query rows per wave (MFMA N dimension)
 constexpr int kMaxNodes = 256;
+constexpr int kMaxPrefix = 0x7FFFFFFF - 4 * kMaxNodes;   // tokens: positions, those of tiles behind it too, are ints
 constexpr int kMaxBatchAttn = 1024;
 constexpr int kMaxBatchShared = 512; // shared-prefix attention: the LDS tables of sequences and groups
 constexpr int kMaxGroups = 256;

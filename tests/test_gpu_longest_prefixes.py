@@ -43,6 +43,21 @@ def test_a_window_at_the_end_of_the_longest_table(which, N, D, P, back):
              f"{which} {N} {P} {back}")
 
 
+@pytest.mark.parametrize("N", [1, 40])
+@pytest.mark.parametrize("P,columns", [(256, 1 << 23), (256, (1 << 24) + 3), (16, 1 << 27)])
+def test_a_table_with_room_for_more_tokens_than_a_prefix_can_have(N, P, columns):
+    T = U.require_gpu()
+    w = LU.workload(72, B=1, N=N, Hq=8, Hkv=2, D=128, P=P, lens=[777])
+    print(f"N {N} P {P} columns {columns}", flush=True)
+    d = U.upload(w)
+    table = torch.full((1, columns), -1, dtype=torch.int32, device="cuda")
+    table[:, :w.page_table.shape[1]] = d["page_table"]
+    out, lse = T.tree_verify_attention(d["q"], d["k_tree"], d["v_tree"], d["k_cache"], d["v_cache"], table, d["kv_len"],
+                                       d["parent"], max_kv_len=777)
+    want, z = U.gpu_attention(T, w, d=d)
+    assert np.array_equal(U.bf16_to_f64(out), want) and np.array_equal(lse.cpu().numpy(), z)
+
+
 @pytest.mark.parametrize("shared", [False, True])
 def test_a_prefix_of_nearly_2_to_the_31_tokens(shared):
     """All pages but the last 390 are one page of zeros (weight 1 each); those hold keys of

@@ -15,6 +15,12 @@ SOURCE = """
 #include "tree_attention_common.h"
 #define API extern "C" __attribute__((visibility("default")))
 API int page_window_end(int first, int p_shift) { return tv::page_window_end(first, p_shift); }
+API int clamp_len(int L, int max_pages, int p_shift) {
+    tv::AttnParams p{};
+    p.max_pages = max_pages;
+    p.p_shift = p_shift;
+    return tv::clamp_len(L, p);
+}
 """
 
 
@@ -47,3 +53,15 @@ def test_sub_ranges_of_a_piece_reach_its_end(host, shift, back):
             end = host.page_window_end(first, shift)
             assert end == (first + CACHED) * P // KEYS and end > t
             t = min(end, tiles)
+
+
+@pytest.mark.parametrize("shift", range(9))
+def test_lengths_are_those_of_the_table_whatever_its_size(host, shift):
+    """A table may have room for more tokens than a prefix can have."""
+    for columns in (1, 3, (LONGEST >> shift) + 1, (1 << 31 - shift) - 1, 1 << 31 - shift, (1 << 32 - shift) + 5,
+                    (1 << 31) - 1):
+        if columns >= 1 << 31:
+            continue
+        room = min(columns << shift, LONGEST)
+        for L in (-5, 0, 1, 7, 300, 0x7FFFFFC0, 0x7FFFFFFF, LONGEST, LONGEST + 1):
+            assert host.clamp_len(L, columns, shift) == min(max(L, 0), room), (columns, L)
