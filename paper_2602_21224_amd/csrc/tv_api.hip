@@ -364,18 +364,24 @@ constexpr int kKv4StreamWgPerCu = 2;
 
 struct Kv4Shape : AttnShape {
     bool stream;
-    int max_wg;
+    int max_wg, setup;
 };
 
-Kv4Shape kv4_shape(int N, int Hq, int Hkv, long prefix) {
+Kv4Shape kv4_shape(int N, int Hq, int Hkv, bool stream) {
     Kv4Shape s;
     static_cast<AttnShape &>(s) = attn_shape(N, Hq, Hkv);
-    s.stream = s.rows <= kv4_stream_rows(prefix);
+    s.stream = stream;
+    s.setup = stream ? kKv4StreamSetupTiles : kSetupTiles;
     s.max_wg = cu_count() * (s.stream ? kKv4StreamWgPerCu : kWgPerCu);
     s.rows_per_block = s.stream ? (s.rows <= 16 ? 16 : 32) : s.rows <= 128 ? 128 : 256;
     s.row_blocks = (s.rows + s.rows_per_block - 1) / s.rows_per_block;
     s.tree_tiles_all = s.row_blocks * ((N + tv::kKeyTile - 1) / tv::kKeyTile);      // at most
     return s;
+}
+
+// Virtual tiles of such a launch over `tiles` prefix tiles.
+long kv4_tiles(const Kv4Shape &s, int B, int Hkv, long tiles) {
+    return (long)B * Hkv * ((long)s.row_blocks * (tiles + s.setup) + s.tree_tiles_all);
 }
 
 }  // namespace
@@ -734,11 +740,11 @@ int tree_verify_attention_window(const uint16_t *q, const uint16_t *k_tree, cons
 
 size_t tv_kv4_attention_workspace_size(int B, int N, int Hq, int Hkv, int D) {
     if (!attn_shape_ok(B, N, Hq, Hkv, D)) return 0;
-    size_t need = 0;
-    for (long prefix : {0L, (long)INT_MAX}) {       // the most rows to either kernel
-        const Kv4Shape s = kv4_shape(N, Hq, Hkv, prefix);
+    size_t need = 0;                                // of either kernel: lengths and tables choose
+    for (bool stream : {false, true}) {
+        const Kv4Shape s = kv4_shape(N, Hq, Hkv, stream);
         const size_t n = attn_workspace(s, D, s.max_wg, true).total;
-        if (need < n) need = n;
+        if (need < n && (!stream || s.rows <= kv4_stream_rows(LONG_MAX))) need = n;
     }
     return need;
 }
@@ -759,13 +765,14 @@ int tree_verify_attention_kv4(const uint16_t *q, const uint16_t *k_tree, const u
     if (workspace_bytes < tv_kv4_attention_workspace_size(B, N, Hq, Hkv, D)) return TV_ERR_WORKSPACE;
     const long max_len = (long)max_pages * P;
     const long tiles = window_tiles(max_kv_len < max_len ? max_kv_len : max_len, window, sinks);
-    const Kv4Shape s = kv4_shape(N, Hq, Hkv, tiles * tv::kKeyTile);
+    // what the window call accepts; where the lengths that the table has room for are too many
+    // tiles in blocks of few rows, larger blocks are taken
+    const AttnShape plain = attn_shape(N, Hq, Hkv);
+    if (attn_tiles(plain, B, Hkv, max_len) >= kMaxTiles) return TV_ERR_SHAPE;
+    Kv4Shape s = kv4_shape(N, Hq, Hkv, plain.rows <= kv4_stream_rows(tiles * tv::kKeyTile));
+    if (s.stream && kv4_tiles(s, B, Hkv, (max_len + tv::kKeyTile - 1) / tv::kKeyTile) >= kMaxTiles)
+        s = kv4_shape(N, Hq, Hkv, false);
     const AttnWorkspace ws = attn_workspace(s, D, s.max_wg, true);
-    const int setup = s.stream ? kKv4StreamSetupTiles : kSetupTiles;
-    auto tiles_of = [&](long prefix) {
-        return (long)B * Hkv * ((long)s.row_blocks * (prefix + setup) + s.tree_tiles_all);
-    };
-    if (tiles_of((max_len + tv::kKeyTile - 1) / tv::kKeyTile) >= kMaxTiles) return TV_ERR_SHAPE;
     if (!device_ok()) return TV_ERR_DEVICE;
 
     tv::Kv4AttnParams p{};
@@ -773,11 +780,11 @@ int tree_verify_attention_kv4(const uint16_t *q, const uint16_t *k_tree, const u
                   window, sinks, scale, out, lse, workspace, ws);
     p.k4 = k4; p.v4 = v4; p.scales = scales;
     p.g_inv = s.G == 1 ? 0u : (unsigned)((1ull << 32) / (unsigned)s.G + 1);
-    long num_wg = tiles_of(tiles) / (s.stream ? kKv4StreamMinShareTiles : kMinShareTiles);
+    long num_wg = kv4_tiles(s, B, Hkv, tiles) / (s.stream ? kKv4StreamMinShareTiles : kMinShareTiles);
     if (num_wg < 1) num_wg = 1;
     if (num_wg > s.max_wg) num_wg = s.max_wg;
     p.rows_per_block = s.rows_per_block;
-    p.setup_tiles = setup;
+    p.setup_tiles = s.setup;
     p.num_wg = (int)num_wg;
     return tv::launch_kv4_attention(p, D, stream) == hipSuccess ? TV_OK : TV_ERR_HIP;
 }

@@ -58,6 +58,22 @@ def test_a_table_with_room_for_more_tokens_than_a_prefix_can_have(N, P, columns)
     assert np.array_equal(U.bf16_to_f64(out), want) and np.array_equal(lse.cpu().numpy(), z)
 
 
+@pytest.mark.parametrize("window,sinks", [(0, 0), (600, 5)])
+@pytest.mark.parametrize("N,Hq,L", [(12, 96, 300), (12, 96, 2500), (40, 48, 2500), (1, 24, 700)])
+def test_4_bits_in_a_table_for_more_row_blocks_than_are_counted(N, Hq, L, window, sinks):
+    """24 KV heads in a table of nearly 2^31 tokens: blocks of 32 rows would be too many tiles."""
+    T = U.require_gpu()
+    w = LU.workload(73, B=1, N=N, Hq=Hq, Hkv=24, D=64, P=256, lens=[L], window=window, sinks=sinks)
+    print(f"N {N} Hq {Hq} L {L} window {window}", flush=True)
+    d, bits = U.upload(w), LU.cache4(w)
+    table = torch.full((1, LONGEST // 256), -1, dtype=torch.int32, device="cuda")
+    table[:, :w.page_table.shape[1]] = d["page_table"]
+    out, lse = T.tree_verify_attention_kv4(d["q"], d["k_tree"], d["v_tree"], *[U.dev(a) for a in bits], table, d["kv_len"],
+                                           d["parent"], max_kv_len=L, window=window, sinks=sinks)
+    LU.check(w, U.bf16_to_f64(out), lse.cpu().numpy().astype(np.float64), LU.expected(w, window, sinks, bits),
+             f"{N} {Hq} {L} {window}")
+
+
 @pytest.mark.parametrize("shared", [False, True])
 def test_a_prefix_of_nearly_2_to_the_31_tokens(shared):
     """All pages but the last 390 are one page of zeros (weight 1 each); those hold keys of
