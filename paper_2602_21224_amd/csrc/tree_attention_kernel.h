@@ -462,9 +462,7 @@ __global__ __launch_bounds__(NW * kWave) void tree_attention_kernel(
                 } else {
                     const int rloc = wave_u * kRowsPerWave + col;
                     float *pm = p.ws_ml + ((size_t)slot * p.rows_per_block + rloc) * (FINE ? 4 : 2);
-                    pm[0] = WIN                      ? part_max(st.m_run, l_tot, p.scale_log2)
-                            : st.m_run == kNegInf ? kNegInf
-                                                  : st.m_run * p.scale_log2;
+                    pm[0] = part_max(st.m_run, l_tot, p.scale_log2);
                     pm[1] = l_tot;
                     if constexpr (FINE) pm[2] = unscale;
                 }
@@ -540,7 +538,7 @@ __global__ __launch_bounds__(NW * kWave) void tree_attention_kernel(
                     *reinterpret_cast<bf16x8 *>(p.ws_o + ((size_t)slot * p.rows_per_block + r) * D + ch * 8) = o;
                     if (ch == 0) {
                         float *pm = p.ws_ml + ((size_t)slot * p.rows_per_block + r) * (FINE ? 4 : 2);
-                        pm[0] = WIN ? part_max(M, Lsum, c) : (M == kNegInf) ? kNegInf : M * c;
+                        pm[0] = part_max(M, Lsum, c);
                         pm[1] = Lsum;
                         if constexpr (FINE) pm[2] = unscale;
                     }

@@ -404,7 +404,7 @@ __device__ __forceinline__ void own_shares(const SharedAttnParams &p, int wid, i
                     *reinterpret_cast<bf16x4 *>(o + db * 16 + 4 * g4) = v;
                 }
                 if (g4 == 0) {
-                    const float m2 = st.m[rt] == kNegInf ? kNegInf : st.m[rt] * c;
+                    const float m2 = part_max(st.m[rt], l, c);
                     if (!last) (whole ? p.ws_row + all + row : p.own_piece + piece)[0] = f32x4{m2, l, unscale, 0.f};
                     else if (p.lse) p.lse[row] = (m2 + __builtin_amdgcn_logf(l)) * kLn2;
                 }

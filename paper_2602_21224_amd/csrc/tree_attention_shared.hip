@@ -575,7 +575,7 @@ __global__ __launch_bounds__(NT) void shared_attention_kernel(SharedAttnParams p
             }
         }
         if (half == 0) {
-            const float m2 = (st.m_run == kNegInf) ? kNegInf : st.m_run * p.scale_log2;
+            const float m2 = part_max(st.m_run, l_tot, p.scale_log2);
             const f32x4 desc = {m2, l_tot, unscale, 0.f};
             const size_t at = (size_t)qnode * p.Hq + hq;
             if (!complete) p.ws_piece[(size_t)slot * p.rows_per_block + wave_u * kRowsPerWave + col] = desc;
