@@ -250,9 +250,10 @@ __device__ __forceinline__ float part_max(float m, float l, float c) {
 // Exclusive prefix sum of per-sequence tile counts into g_cum[0..B], the
 // clamped prefix lengths into g_len[0..B) and the node counts into g_nn:
 // wave 0 reads kv_len (and num_nodes) once per lane and scans with cross-lane
-// shifts, one barrier for the whole workgroup.
-template <int NT, typename Params>
-__device__ void build_cumulative(const Params &p) {
+// shifts, one barrier for the whole workgroup. tiles(L, nodes) counts a sequence's
+// virtual tiles, as the caller's search for a piece adds them up.
+template <typename Tiles>
+__device__ void build_cumulative(const AttnParams &p, Tiles tiles) {
     if (threadIdx.x < kWave) {
         const int lane = threadIdx.x;
         int carry = 0;
@@ -260,7 +261,7 @@ __device__ void build_cumulative(const Params &p) {
             const int b = b0 + lane;
             const int L = b < p.B ? clamp_len(p.kv_len[b], p) : 0;
             const int nb = b < p.B ? nodes_of(b, p) : 0;
-            const int t = b < p.B ? tiles_of_sequence(L, nb, p) : 0;
+            const int t = b < p.B ? tiles(L, nb) : 0;
             int x = t;                                   // inclusive scan over the wave
             #pragma unroll
             for (int off = 1; off < kWave; off <<= 1) {

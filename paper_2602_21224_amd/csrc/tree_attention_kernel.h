@@ -33,7 +33,7 @@ __global__ __launch_bounds__(NW * kWave) void tree_attention_kernel(
     const int col = lane & 31;
     const int w = xcd_contiguous_id(blockIdx.x, p.num_wg);
 
-    build_cumulative<NT>(p);
+    build_cumulative(p, [&](int L, int nodes) { return tiles_of_sequence(L, nodes, p); });
 
     const int total = g_cum[p.B];
     // Workgroup u < nw takes virtual tiles [share_start(u), share_start(u + 1)):

@@ -27,7 +27,8 @@ __device__ __forceinline__ int head_tiles(const Kv4AttnParams &p, int ntp, int n
     for (int rb = 0; rb * p.rows_per_block < nodes * p.G; ++rb) t += p.setup_tiles + ntp + tree_tiles(p, rb, nodes);
     return t;
 }
-__device__ __forceinline__ int tiles_of_sequence(int L, int nodes, const Kv4AttnParams &p) {
+// Those of a sequence with a prefix of L tokens.
+__device__ __forceinline__ int sequence_tiles(const Kv4AttnParams &p, int L, int nodes) {
     return p.Hkv * head_tiles(p, (L + KT - 1) / KT - span_of(L, p).gap, nodes);
 }
 

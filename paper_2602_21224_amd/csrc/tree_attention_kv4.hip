@@ -249,7 +249,7 @@ __global__ __launch_bounds__(kStreamWaves * kWave, kStreamWgPerCu) void kv4_stre
     const int w = xcd_contiguous_id(blockIdx.x, p.num_wg);
     unsigned char *vhalf = g_half + wave_u * (Gm::kTileBytes / 2);
 
-    build_cumulative<NT>(p);
+    build_cumulative(p, [&](int L, int nodes) { return sequence_tiles(p, L, nodes); });
 
     const Shares sh(g_cum[p.B], p.num_wg);
     const int start = sh.start_of(w), end = sh.start_of(w + 1);

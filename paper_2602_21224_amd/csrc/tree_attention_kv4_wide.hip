@@ -90,7 +90,7 @@ __global__ __launch_bounds__(NW * kWave) void kv4_wide_kernel(Kv4AttnParams p) {
     const int half = lane >> 5, col = lane & 31;
     const int w = xcd_contiguous_id(blockIdx.x, p.num_wg);
 
-    build_cumulative<NT>(p);
+    build_cumulative(p, [&](int L, int nodes) { return sequence_tiles(p, L, nodes); });
 
     const Shares sh(g_cum[p.B], p.num_wg);
     const int start = sh.start_of(w), end = sh.start_of(w + 1);

@@ -2,6 +2,8 @@
 their own headers (CPU only)."""
 import ctypes
 import os
+import re
+import shutil
 import subprocess
 
 import pytest
@@ -65,3 +67,23 @@ def test_lengths_are_those_of_the_table_whatever_its_size(host, shift):
         room = min(columns << shift, LONGEST)
         for L in (-5, 0, 1, 7, 300, 0x7FFFFFC0, 0x7FFFFFFF, LONGEST, LONGEST + 1):
             assert host.clamp_len(L, columns, shift) == min(max(L, 0), room), (columns, L)
+
+
+@pytest.mark.parametrize("source", ["tree_attention_kv4.hip", "tree_attention_kv4_wide.hip"])
+def test_the_scan_of_lengths_counts_the_units_that_the_search_walks(source, tmp_path):
+    """Over 4 bits the cumulative tiles of a batch come from the function whose terms the
+    search for a piece adds up: without it the kernels do not compile."""
+    from paper_2602_21224_amd import build
+    if not os.path.exists(build.HIPCC):
+        pytest.skip("hipcc not available")
+    shutil.copytree(CSRC, tmp_path / "csrc", ignore=shutil.ignore_patterns("*.so", "*.o"))
+    header = tmp_path / "csrc" / "tree_attention_kv4.h"
+    text, found = re.subn(r"\{\s*return p\.Hkv \* head_tiles\([^;]*;\s*\}", "= delete;", header.read_text())
+    assert found == 1
+    cmd = [build.HIPCC, *[f for f in build.FLAGS if f != "-O3"], "-fsyntax-only", "--offload-host-only",
+           str(tmp_path / "csrc" / source)]
+    with_it = subprocess.run(cmd, capture_output=True, text=True)
+    assert with_it.returncode == 0, with_it.stderr[-2000:]
+    header.write_text(text)
+    without = subprocess.run(cmd, capture_output=True, text=True)
+    assert without.returncode != 0 and "deleted function" in without.stderr
