@@ -140,7 +140,7 @@ __device__ __forceinline__ int tiles_of_sequence(int L, int nodes, const AttnPar
 struct Span {
     int lo0, lo, sinks, ns, gap;
 };
-__device__ __forceinline__ Span span_of(int L, const WindowAttnParams &p) {
+__host__ __device__ __forceinline__ Span span_of(int L, const WindowAttnParams &p) {
     Span s;
     s.lo0 = p.window > 0 ? L - p.window + 1 : -kMaxNodes;
     s.lo = max(s.lo0, 0);
@@ -155,29 +155,31 @@ __device__ __forceinline__ int tiles_of_sequence(int L, int nodes, const WindowA
 }
 
 // Steps from node i to its root (the ancestor sets are reflexive).
-__device__ __forceinline__ int depth_of(const unsigned long long (&anc)[4]) {
-    return __popcll(anc[0]) + __popcll(anc[1]) + __popcll(anc[2]) + __popcll(anc[3]) - 1;
+__host__ __device__ __forceinline__ int depth_of(const unsigned long long (&anc)[4]) {
+    return __builtin_popcountll(anc[0]) + __builtin_popcountll(anc[1]) + __builtin_popcountll(anc[2]) +
+           __builtin_popcountll(anc[3]) - 1;
 }
 // Keys of the prefix tile at position `base` that the node with ancestor set `anc` sees. A piece
 // whose tiles end before the window has no ancestor sets: for it, only the sinks count.
-__device__ __forceinline__ unsigned long long window_bits(const Span &sp, int base, const unsigned long long (&anc)[4]) {
+__host__ __device__ __forceinline__ unsigned long long window_bits(const Span &sp, int base,
+                                                                   const unsigned long long (&anc)[4]) {
     const int d = base + KT > sp.lo0 ? depth_of(anc) : 0;
     const int from = min(max(sp.lo0 + d - base, 0), KT), to = min(max(sp.sinks - base, 0), KT);
     return (from < KT ? ~0ull << from : 0ull) | (to < KT ? (1ull << to) - 1ull : ~0ull);
 }
 // Whether every node of a sequence of at most N sees all of that tile.
-__device__ __forceinline__ bool window_clear(const Span &sp, int base, int N) {
+__host__ __device__ __forceinline__ bool window_clear(const Span &sp, int base, int N) {
     return base >= sp.lo0 + N - 1 || base + KT <= sp.sinks;
 }
 // Word w of a node's root path as far as the window shows it: an ancestor's place among the
 // path's nodes is its depth, and its position L + depth.
-__device__ __forceinline__ unsigned long long window_path(const unsigned long long (&anc)[4], int w, int L,
-                                                          const WindowAttnParams &p) {
+__host__ __device__ __forceinline__ unsigned long long window_path(const unsigned long long (&anc)[4], int w, int L,
+                                                                   const WindowAttnParams &p) {
     unsigned long long x = anc[w];
     const int first = max(p.sinks - L, 0), last = depth_of(anc) - p.window;      // depths not seen
     if (p.window <= 0 || last < first) return x;
     int d = 0;
-    for (int u = 0; u < w; ++u) d += __popcll(anc[u]);
+    for (int u = 0; u < w; ++u) d += __builtin_popcountll(anc[u]);
     unsigned long long seen = 0;
     for (; x; x &= x - 1, ++d)
         if (d < first || d > last) seen |= x & -x;
