@@ -439,9 +439,10 @@ TV_API int tree_verify_attention_window(const uint16_t *q, const uint16_t *k_tre
  *   scales   [num_pages, Hkv, P, 2, D/32] uint8: of each block of the K row,
  *            then of the V row, the exponent e of its power of two plus 127.
  *            255: every value of the block is NaN.
- * A value is its code's times 2^e; every one is exact in bf16 (from 2^128 on,
- * which kv4_write does not make, it is infinite). Tokens of a page lie together
- * per KV head: [Hkv, P], not [P, Hkv] as in the bf16 cache.
+ * A value is its code's times 2^e; every one is exact in bf16, subnormal ones too,
+ * which the attention takes as they are (from 2^128 on, which kv4_write does not
+ * make, it is infinite). Tokens of a page lie together per KV head: [Hkv, P], not
+ * [P, Hkv] as in the bf16 cache.
  * ------------------------------------------------------------------------
  * kv4_write
  *
