@@ -34,7 +34,9 @@
 // 90 instead of 80 and 36 instead of 33.
 // The registers that held a tile's codes of K take the next tile's as soon as its scores are
 // under way, those of V when V is in LDS: loads are on their way for most of a tile's time, and
-// with two sets of registers (a set more in flight) a wave spilled.
+// with two sets of registers (a set more in flight) a wave spilled. (Of the instances, those for 32
+// rows of head size 128 spill 4 registers, 11 with pages of fewer than 16 keys: in the set-up of
+// trees of more than 64 nodes, not in the tiles.)
 #include "tree_attention_kv4.h"
 
 namespace tv {

@@ -352,7 +352,10 @@ void window_params(tv::WindowAttnParams &p, const uint16_t *q, const uint16_t *k
 // and 57 (every block takes the tree's tiles again); 16 sequences of 500-900 tokens, 96 rows 35
 // and 32; of 1024-4096 tokens, 64 rows 41 and 62, 96 rows 51 and 63, 128 rows 63 and 64, 160 rows
 // 73 and 67; 4 sequences of 32768 tokens, 128 rows 115 and 154, 160 rows 142 and 165, 192 rows
-// 162 and 166.
+// 162 and 166. Head size 64 has its line in nearly the same place: 64 sequences of 200-500 tokens,
+// 64 rows 35 and 42, 68 rows 43 and 42; 16 of 500-900, 64 rows 21.1 and 23.4, 96 rows 24.1 both; of
+// 1024-4096, 96 rows 36 and 45, 128 rows 44 and 46, 160 rows 51 both; 4 of 32768, 160 rows 95 and
+// 117, 192 rows 110 and 118 (the line costs it 4 and 7 % at 128 and 192 rows).
 // Shares: of 2, 4, 6, 8 and 12 set-up tiles per unit and 4, 6 and 8 tiles at least per share the
 // smallest calls took 17.3 to 13.3, 8 and 8 13.8, the larger ones the same within their noise.
 constexpr int kv4_stream_rows(long prefix) {
